@@ -315,6 +315,215 @@ trevs_status trevs_topk_select(const float* scores, int32_t B, int32_t N, int32_
                                int32_t* kept_idx, void* workspace, size_t workspace_bytes,
                                void* stream);
 
+/* ------------------------------------------------------------------------
+ * Rotary positions of query and key rows (the positions that stage 2 compacts
+ * without renumbering them).  For token (b,s), pair i < R/2 of the first
+ * R = rot_dim values of every head, with a, b the pair's values:
+ *   w  = 2 pi * pos[plane(i)][b][s] * freqs[i]
+ *   a' = attn_factor (a cos w - b sin w),  b' = attn_factor (b cos w + a sin w)
+ * A pair is values (i, i + R/2) of the head, or (2i, 2i+1) with `interleaved`.
+ * plane(i) deals the pairs to the n_pos position planes in order: the first
+ * section[0] pairs use plane 0, the next section[1] plane 1, and so on.
+ * Values past R are copied.  `inverse` turns by -w instead (with the same
+ * attn_factor): the gradient of the rotation, and with attn_factor 1 its undoing.
+ * The turns pos * freqs and their fraction are formed in 64 bits, sine and
+ * cosine of the fraction in 32; positions are exact up to 2^53.
+ * ---------------------------------------------------------------------- */
+#define TREVS_MAX_POS_PLANES 4
+typedef struct trevs_rope_args {
+  uint32_t struct_size;      /* sizeof(trevs_rope_args) */
+  int32_t B, S;              /* samples, rows of each */
+  int32_t H_q, H_k;          /* heads of q and k; 0 leaves that tensor out (not both) */
+  int32_t d_head;            /* 64, 128 or 256 */
+  int32_t rot_dim;           /* R: a multiple of 16, 16..d_head */
+  int32_t n_pos;             /* position planes, 1..TREVS_MAX_POS_PLANES */
+  int32_t section[TREVS_MAX_POS_PLANES]; /* pairs of each plane, >= 0; the first n_pos sum to R/2 */
+  int32_t interleaved;       /* 0: pairs (i, i + R/2); 1: pairs (2i, 2i+1) */
+  int32_t inverse;           /* 1: turn by -w */
+  int32_t dtype;             /* trevs_dtype of q, k and their outputs */
+  float attn_factor;         /* finite; normally 1 */
+  const double* freqs;       /* [R/2] turns per position, on the device (trevs_rope_frequencies) */
+  const int64_t* pos;        /* [n_pos,B,S] */
+  const void* q;             /* [B,S,H_q,d_head], rows q_ld elements apart (16-byte aligned) */
+  const void* k;             /* [B,S,H_k,d_head], rows k_ld elements apart (16-byte aligned) */
+  void* q_out;               /* OUT as q, rows q_out_ld apart; may be q itself (in place) */
+  void* k_out;               /* OUT as k, rows k_out_ld apart; may be k itself (in place) */
+  int64_t q_ld, k_ld;        /* elements from one row to the next, 0 = H * d_head; row bytes % 16 == 0 */
+  int64_t q_out_ld, k_out_ld;
+} trevs_rope_args;
+
+trevs_status trevs_rope(const trevs_rope_args* args, void* stream);
+
+/* The frequencies of trevs_rope, computed on the host into freqs [rot_dim/2]
+ * (host memory): f_i = base^(-2i/rot_dim) / (2 pi) turns per position, for
+ * contexts longer than the model's own divided by `factor`
+ *   NONE    not at all
+ *   LINEAR  in every pair (the positions are interpolated)
+ *   PARTS   by parts (arxiv 2309.00071, Sec. 3.2): with r = original_len * f_i
+ *           turns over the original context, pairs with r >= beta_fast not at
+ *           all, with r <= beta_slow in full, between them in proportion. */
+typedef enum trevs_rope_scaling {
+  TREVS_ROPE_NONE = 0,
+  TREVS_ROPE_LINEAR = 1,
+  TREVS_ROPE_PARTS = 2
+} trevs_rope_scaling;
+trevs_status trevs_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
+                                    double original_len, double beta_fast, double beta_slow,
+                                    double* freqs);
+
+/* ------------------------------------------------------------------------
+ * A paged K/V cache held in 8 bits: what the layers after the pruning, and
+ * the decode steps, attend to.  Tokens live in pages of page_tokens; every
+ * page holds, for each layer and KV head, one block of keys and one of
+ * values as OCP e4m3 numbers with one scale each:
+ *   key   of token t, channel c = k[layer][page][h][t][c] * k_scale[layer][page][h]
+ *   value of token t, channel c = v[layer][page][h][c][t] * v_scale[layer][page][h]
+ * (values are stored with the token last).  A scale is a power of two,
+ * 2^-126..2^120: the smallest s with |x| <= 448 s over the block when its rows
+ * were written, so that dividing by it is exact and a value is rounded once,
+ * to the nearest e4m3 (ties to even).  Rows appended to a block that already
+ * holds tokens keep its scale or raise it; when it rises, the block's earlier
+ * values are rounded again to the new scale (exact above its subnormals).
+ *
+ * One page table serves every layer: sequence slot i < n_slots holds len[i]
+ * tokens, token t in page table[i][t / page_tokens].  ref[p] counts the slots
+ * that hold page p; 0 means free.  Slots may share pages (trevs_pages_fork);
+ * a shared page is only read: trevs_pages_reserve gives a slot its own copy
+ * of a shared last page before rows are appended to it.
+ * An empty table is: len and ref all 0 (table entries past a slot's pages
+ * are not read; the page operations leave -1 there).  All arrays are the
+ * caller's, in device memory.  Table entries outside 0..n_pages-1 are taken
+ * as absent (read as masked, never written), slots outside 0..n_slots-1 as
+ * empty, and lengths are clamped into 0..max_pages * page_tokens.
+ * ---------------------------------------------------------------------- */
+typedef struct trevs_kv8_cache {
+  uint32_t struct_size;      /* sizeof(trevs_kv8_cache) */
+  int32_t n_layers;          /* >= 1 */
+  int32_t n_pages;           /* >= 1 */
+  int32_t page_tokens;       /* 16, 32 or 64 */
+  int32_t H_kv;              /* KV heads */
+  int32_t d_head;            /* 64, 128 or 256 */
+  int32_t n_slots;           /* sequences */
+  int32_t max_pages;         /* pages of the longest sequence; max_pages * page_tokens <= 2^30 */
+  uint8_t* k;                /* [n_layers,n_pages,H_kv,page_tokens,d_head] e4m3 (16-byte aligned) */
+  uint8_t* v;                /* [n_layers,n_pages,H_kv,d_head,page_tokens] e4m3 (16-byte aligned) */
+  float* k_scale;            /* [n_layers,n_pages,H_kv] */
+  float* v_scale;            /* [n_layers,n_pages,H_kv] */
+  int32_t* table;            /* [n_slots,max_pages] */
+  int32_t* len;              /* [n_slots] */
+  int32_t* ref;              /* [n_pages] */
+} trevs_kv8_cache;
+
+/* Page operations.  Every list below has n entries, n in
+ * 1..TREVS_MAX_PAGE_REQUESTS, in device memory; a list of slots that is NULL
+ * stands for 0..n-1 (n <= n_slots).  Results are those of serving the
+ * requests in order.  A request that names a slot out of range, or the slot
+ * that an earlier request of the call names (as its destination, in a fork),
+ * does nothing.  The calls only change table, len and ref; a call must not run
+ * beside another one on the same cache. */
+#define TREVS_MAX_PAGE_REQUESTS 1024
+
+/* Room for n_new[i] more tokens in slots[i]: its length grows by that and its
+ * table by the pages needed, the lowest free ones first, in ascending order.
+ * When the slot's last page is shared and not full, the first of them
+ * replaces it: copy_src[i] and copy_dst[i] are then the shared page and its
+ * replacement, for trevs_kv8_copy_pages, else both are -1.  A request that
+ * the free pages or max_pages do not cover, or with n_new[i] < 1, changes
+ * nothing; granted[i] is n_new[i] or 0. */
+trevs_status trevs_pages_reserve(const trevs_kv8_cache* cache, int32_t n, const int32_t* slots,
+                                 const int32_t* n_new, int32_t* granted, int32_t* copy_src,
+                                 int32_t* copy_dst, void* stream);
+
+/* Slot dst[i], which must be empty, shares the pages of the first n_tokens[i]
+ * tokens (clamped into 0..len) of slot src[i], or of all of them with n_tokens
+ * NULL.  A source that is a destination of the same call is refused.  done[i]
+ * is 1, or 0 when the request did nothing. */
+trevs_status trevs_pages_fork(const trevs_kv8_cache* cache, int32_t n, const int32_t* src, const int32_t* dst,
+                              const int32_t* n_tokens, int32_t* done, void* stream);
+
+/* Slot slots[i] keeps its first keep[i] tokens (clamped into 0..len), or none
+ * with keep NULL, and gives up its other pages; pages that no slot holds any
+ * more are free. */
+trevs_status trevs_pages_free(const trevs_kv8_cache* cache, int32_t n, const int32_t* slots,
+                              const int32_t* keep, void* stream);
+
+/* Pages src[i] copied to pages dst[i] in every layer, keys, values and scales
+ * (bit copies); pairs with an entry out of range are skipped.  No page may be
+ * the destination of two pairs, nor of one and the source of another.  n is
+ * not limited here. */
+trevs_status trevs_kv8_copy_pages(const trevs_kv8_cache* cache, int32_t n, const int32_t* src,
+                                  const int32_t* dst, void* stream);
+
+/* Rows written to one layer of the cache: the last n_new[b] tokens of slot
+ * slots[b] (their room reserved before), token len - n_new + t from row t.
+ * n_new is clamped into 0..min(T_max, len).  The pages written must be held
+ * by that slot alone. */
+typedef struct trevs_kv8_write_args {
+  uint32_t struct_size;      /* sizeof(trevs_kv8_write_args) */
+  int32_t B;                 /* sequences */
+  int32_t T_max;             /* padded rows, >= 1 */
+  int32_t layer;             /* 0..n_layers-1 */
+  int32_t dtype;             /* trevs_dtype of k and v */
+  const void* k;             /* [B,T_max,H_kv,d_head], rows k_ld elements apart (16-byte aligned) */
+  const void* v;             /* [B,T_max,H_kv,d_head], rows v_ld elements apart (16-byte aligned) */
+  int64_t k_ld, v_ld;        /* 0 = H_kv * d_head; row bytes % 16 == 0 */
+  const int32_t* n_new;      /* [B], or NULL (= T_max) */
+  const int32_t* slots;      /* [B], or NULL (= 0..B-1, B <= n_slots); no slot twice */
+} trevs_kv8_write_args;
+
+trevs_status trevs_kv8_write(const trevs_kv8_cache* cache, const trevs_kv8_write_args* args, void* stream);
+
+/* Attention of query rows over one layer of the cache.  With L = len[slot],
+ * query row t < q_len[b] of head h sees the keys j of KV head h/G, G = H_q/H_kv,
+ *   causal: j <= L - q_len[b] + t (the rows are the sequence's last ones)
+ *   else:   every j < L
+ *   out[b,t,h,:] = sum_j softmax_j(scale q . k_j) v_j
+ *   lse[b,h,t]   = logsumexp_j(scale q . k_j), natural log
+ * A row that sees no key gives zeros and -inf.  Rows t >= q_len[b] are left as
+ * they were.  Products run on the matrix cores with 32-bit sums: bf16 queries
+ * and attention weights as bf16, fp32 ones as three bf16 parts each. */
+typedef struct trevs_kv8_attention_args {
+  uint32_t struct_size;      /* sizeof(trevs_kv8_attention_args) */
+  int32_t B;                 /* sequences */
+  int32_t T_max;             /* padded query rows, >= 1 */
+  int32_t H_q;               /* query heads; H_q % H_kv == 0 */
+  int32_t layer;             /* 0..n_layers-1 */
+  int32_t dtype;             /* trevs_dtype of q and out */
+  int32_t causal;            /* 0 or 1 */
+  int32_t kv_max;            /* no sequence of the call is longer (longer ones are cut there);
+                                0 = max_pages * page_tokens.  Sizes the launch and the workspace. */
+  float scale;               /* logit scale > 0, normally 1/sqrt(d_head) */
+  const void* q;             /* [B,T_max,H_q,d_head], rows q_ld elements apart (16-byte aligned) */
+  int64_t q_ld;              /* 0 = H_q * d_head; row bytes % 16 == 0 */
+  const int32_t* q_len;      /* [B], clamped into 0..T_max, or NULL (= T_max) */
+  const int32_t* slots;      /* [B], or NULL (= 0..B-1, B <= n_slots) */
+  void* out;                 /* OUT [B,T_max,H_q,d_head] (16-byte aligned) */
+  float* lse;                /* OPTIONAL OUT [B,H_q,T_max] */
+} trevs_kv8_attention_args;
+
+size_t trevs_kv8_attention_workspace_size(const trevs_kv8_cache* cache, const trevs_kv8_attention_args* args);
+trevs_status trevs_kv8_attention(const trevs_kv8_cache* cache, const trevs_kv8_attention_args* args,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* The compaction of trevs_inllm_prune inside the cache, in every layer: with
+ * L = len[src_slots[b]], rows [0,P) ++ (P + kept_idx[b]) ++ [P+K_in, L) of slot
+ * src_slots[b] become the first L - K_in + n_kept tokens of slot dst_slots[b], in
+ * that order, their blocks rounded to scales of their own.  Rows past
+ * len[dst_slots[b]] are dropped (room is reserved before), and a sample with
+ * L < P + K_in is skipped.  The slots' pages must not meet: a destination is
+ * filled from pages that no destination of the call holds. */
+typedef struct trevs_kv8_compact_args {
+  uint32_t struct_size;      /* sizeof(trevs_kv8_compact_args) */
+  int32_t B;                 /* sequences */
+  int32_t P, K_in;           /* prefix rows and visual rows, as in trevs_inllm_args */
+  int32_t n_kept;            /* 1..K_in */
+  const int32_t* kept_idx;   /* [B,n_kept] (clamped into 0..K_in-1) */
+  const int32_t* src_slots;  /* [B] */
+  const int32_t* dst_slots;  /* [B] */
+} trevs_kv8_compact_args;
+
+trevs_status trevs_kv8_compact(const trevs_kv8_cache* cache, const trevs_kv8_compact_args* args, void* stream);
+
 /* Static description of a status code. */
 const char* trevs_status_string(trevs_status status);
 
@@ -326,6 +535,11 @@ int32_t trevs_keep_count(float ratio, int32_t n);
 size_t trevs_prellm_args_size(void);
 size_t trevs_inllm_args_size(void);
 size_t trevs_sensitivity_args_size(void);
+size_t trevs_rope_args_size(void);
+size_t trevs_kv8_cache_size(void);
+size_t trevs_kv8_write_args_size(void);
+size_t trevs_kv8_attention_args_size(void);
+size_t trevs_kv8_compact_args_size(void);
 
 #ifdef __cplusplus
 }

@@ -26,6 +26,9 @@ INLLM_KERNELS = ("t2v_stats", "head_var", "token_score", "topk", "compaction")
 SENSITIVITY_KERNELS = ("t2v_stats", "head_var", "profile", "", "", "", "sensitivity")
 
 SOFTMAX = {"visual": 0, "causal": 1}  # trevs_softmax
+ROPE_SCALING = {"none": 0, "linear": 1, "parts": 2}  # trevs_rope_scaling
+MAX_POS_PLANES = 4
+MAX_PAGE_REQUESTS = 1024
 
 _STATUS = {0: "ok", 1: "invalid argument", 2: "unsupported", 3: "workspace", 4: "hip error"}
 
@@ -38,6 +41,7 @@ class TrevsError(RuntimeError):
 
 c_int32, c_uint32, c_float, c_void_p, c_size_t = (ctypes.c_int32, ctypes.c_uint32, ctypes.c_float,
                                                    ctypes.c_void_p, ctypes.c_size_t)
+c_int64, c_double = ctypes.c_int64, ctypes.c_double
 
 
 class PrellmArgs(ctypes.Structure):
@@ -75,6 +79,43 @@ class SensitivityArgs(ctypes.Structure):
                 ("q", c_void_p * 2), ("k", c_void_p * 2), ("text_len", c_void_p * 2),
                 ("lse_rest", c_void_p * 2), ("ts", c_void_p), ("profile", c_void_p * 2),
                 ("head_var", c_void_p * 2), ("events", c_void_p), ("softmax", c_int32)]
+
+
+class RopeArgs(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("B", c_int32), ("S", c_int32), ("H_q", c_int32),
+                ("H_k", c_int32), ("d_head", c_int32), ("rot_dim", c_int32), ("n_pos", c_int32),
+                ("section", c_int32 * MAX_POS_PLANES), ("interleaved", c_int32),
+                ("inverse", c_int32), ("dtype", c_int32), ("attn_factor", c_float),
+                ("freqs", c_void_p), ("pos", c_void_p), ("q", c_void_p), ("k", c_void_p),
+                ("q_out", c_void_p), ("k_out", c_void_p), ("q_ld", c_int64), ("k_ld", c_int64),
+                ("q_out_ld", c_int64), ("k_out_ld", c_int64)]
+
+
+class Kv8CacheArgs(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("n_layers", c_int32), ("n_pages", c_int32),
+                ("page_tokens", c_int32), ("H_kv", c_int32), ("d_head", c_int32),
+                ("n_slots", c_int32), ("max_pages", c_int32), ("k", c_void_p), ("v", c_void_p),
+                ("k_scale", c_void_p), ("v_scale", c_void_p), ("table", c_void_p),
+                ("len", c_void_p), ("ref", c_void_p)]
+
+
+class Kv8WriteArgs(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("B", c_int32), ("T_max", c_int32), ("layer", c_int32),
+                ("dtype", c_int32), ("k", c_void_p), ("v", c_void_p), ("k_ld", c_int64),
+                ("v_ld", c_int64), ("n_new", c_void_p), ("slots", c_void_p)]
+
+
+class Kv8AttentionArgs(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("B", c_int32), ("T_max", c_int32), ("H_q", c_int32),
+                ("layer", c_int32), ("dtype", c_int32), ("causal", c_int32), ("kv_max", c_int32),
+                ("scale", c_float), ("q", c_void_p), ("q_ld", c_int64), ("q_len", c_void_p),
+                ("slots", c_void_p), ("out", c_void_p), ("lse", c_void_p)]
+
+
+class Kv8CompactArgs(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("B", c_int32), ("P", c_int32), ("K_in", c_int32),
+                ("n_kept", c_int32), ("kept_idx", c_void_p), ("src_slots", c_void_p),
+                ("dst_slots", c_void_p)]
 
 
 def _torch_empty(shape, dtype, device):
@@ -142,12 +183,38 @@ def lib():
         L.trevs_topk_spearman.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p,
                                           c_void_p, c_void_p, c_size_t, c_void_p]
         L.trevs_topk_spearman.restype = ctypes.c_int
-        L.trevs_prellm_args_size.restype = c_size_t
-        L.trevs_inllm_args_size.restype = c_size_t
-        L.trevs_sensitivity_args_size.restype = c_size_t
-        if (L.trevs_prellm_args_size() != ctypes.sizeof(PrellmArgs)
-                or L.trevs_inllm_args_size() != ctypes.sizeof(InllmArgs)
-                or L.trevs_sensitivity_args_size() != ctypes.sizeof(SensitivityArgs)):
+        L.trevs_rope.argtypes = [ctypes.POINTER(RopeArgs), c_void_p]
+        L.trevs_rope.restype = ctypes.c_int
+        L.trevs_rope_frequencies.argtypes = [c_int32, c_double, c_int32, c_double, c_double, c_double,
+                                             c_double, c_void_p]
+        L.trevs_rope_frequencies.restype = ctypes.c_int
+        cache = ctypes.POINTER(Kv8CacheArgs)
+        L.trevs_pages_reserve.argtypes = [cache, c_int32] + [c_void_p] * 6
+        L.trevs_pages_reserve.restype = ctypes.c_int
+        L.trevs_pages_fork.argtypes = [cache, c_int32] + [c_void_p] * 5
+        L.trevs_pages_fork.restype = ctypes.c_int
+        L.trevs_pages_free.argtypes = [cache, c_int32] + [c_void_p] * 3
+        L.trevs_pages_free.restype = ctypes.c_int
+        L.trevs_kv8_copy_pages.argtypes = [cache, c_int32] + [c_void_p] * 3
+        L.trevs_kv8_copy_pages.restype = ctypes.c_int
+        L.trevs_kv8_write.argtypes = [cache, ctypes.POINTER(Kv8WriteArgs), c_void_p]
+        L.trevs_kv8_write.restype = ctypes.c_int
+        L.trevs_kv8_attention_workspace_size.argtypes = [cache, ctypes.POINTER(Kv8AttentionArgs)]
+        L.trevs_kv8_attention_workspace_size.restype = c_size_t
+        L.trevs_kv8_attention.argtypes = [cache, ctypes.POINTER(Kv8AttentionArgs), c_void_p, c_size_t,
+                                          c_void_p]
+        L.trevs_kv8_attention.restype = ctypes.c_int
+        L.trevs_kv8_compact.argtypes = [cache, ctypes.POINTER(Kv8CompactArgs), c_void_p]
+        L.trevs_kv8_compact.restype = ctypes.c_int
+        for size, struct in ((L.trevs_prellm_args_size, PrellmArgs), (L.trevs_inllm_args_size, InllmArgs),
+                             (L.trevs_sensitivity_args_size, SensitivityArgs),
+                             (L.trevs_rope_args_size, RopeArgs), (L.trevs_kv8_cache_size, Kv8CacheArgs),
+                             (L.trevs_kv8_write_args_size, Kv8WriteArgs),
+                             (L.trevs_kv8_attention_args_size, Kv8AttentionArgs),
+                             (L.trevs_kv8_compact_args_size, Kv8CompactArgs)):
+            size.restype = c_size_t
+            if size() == ctypes.sizeof(struct):
+                continue
             raise RuntimeError("libtrevs.so argument structs do not match this binding")
         _lib = L
     return _lib
@@ -487,6 +554,350 @@ def topk_spearman(sv, st, k, stream=None):
     each sample (Sec. 3).  sv, st [B,N] fp32 on the device.  Returns
     (rho float64 [B], kept_idx int32 [B,k] ascending)."""
     return TopkSpearman(sv, st, k)(stream)
+
+
+# ------------------------------------------------------------- serving cache
+def _row_ld(t, name, device, dtype, heads=None):
+    """Elements from one row of t [B,T,H,d] to the next: heads and channels
+    dense, rows evenly spaced (a slice of a fused projection is)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.dim() != 4 or min(t.shape) < 1:
+        raise ValueError(f"{name} must be a non-empty [B,T,H,d], got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    B, T, H, d = t.shape
+    sb, st, sh, sd = t.stride()
+    ld = st if T > 1 else sb if B > 1 else H * d
+    if sd != 1 or (H > 1 and sh != d) or (B > 1 and sb != T * ld) or ld < H * d:
+        raise ValueError(f"{name} must have dense heads and evenly spaced rows")
+    return ld
+
+
+def _check_list(t, name, device, n=None):
+    if t is None:
+        return
+    _check(t, name, device, 1, torch.int32)
+    if n is not None and t.shape != (n,):
+        raise ValueError(f"{name} must be [{n}]")
+
+
+def _call(fn, device, stream, *args):
+    """fn(*args, stream) on the tensors' device: with torch's current stream
+    there unless one is given."""
+    with torch.cuda.device(device):
+        st = fn(*args, _stream(stream))
+    if st:
+        raise TrevsError(st, fn.__name__)
+
+
+def rope_frequencies(rot_dim, *, base=10000.0, scaling="none", factor=1.0, original_len=0,
+                     beta_fast=32.0, beta_slow=1.0):
+    """Frequencies of Rope, float64 [rot_dim/2] on the host, in turns per
+    position: base^(-2i/rot_dim) / 2 pi; for longer contexts divided by
+    `factor` in every pair (scaling="linear") or by parts ("parts": pairs that
+    turn beta_fast times or more over original_len positions not at all, those
+    of beta_slow or less in full, between them in proportion)."""
+    if scaling not in ROPE_SCALING:
+        raise ValueError(f"scaling must be one of {sorted(ROPE_SCALING)}")
+    out = torch.empty(max(int(rot_dim) // 2, 1), dtype=torch.float64)
+    st = lib().trevs_rope_frequencies(rot_dim, base, ROPE_SCALING[scaling], factor, original_len,
+                                      beta_fast, beta_slow, out.data_ptr())
+    if st:
+        raise TrevsError(st, "trevs_rope_frequencies")
+    return out
+
+
+class Rope:
+    """Rotary positions of query rows q [B,S,H_q,d] and, unless None, key rows
+    k [B,S,H_k,d] at pos [n_pos,B,S] int64, with freqs [R/2] float64 on the
+    device (rope_frequencies).  sections deals the R/2 pairs to the position
+    planes (all to the first by default).  Outputs are allocated once, or are
+    q and k themselves with inplace=True; call() enqueues the rotation and
+    returns (q_out, k_out).  inverse=True turns back: the gradient of the
+    rotation."""
+
+    def __init__(self, q, k, pos, *, freqs, sections=None, interleaved=False, inverse=False,
+                 attn_factor=1.0, inplace=False):
+        self.device = dev = q.device
+        dt = q.dtype
+        a = RopeArgs()
+        a.struct_size = ctypes.sizeof(RopeArgs)
+        a.dtype = _dtype_code(q)
+        a.q_ld = _row_ld(q, "q", dev, dt)
+        a.B, a.S, a.H_q, a.d_head = q.shape
+        if k is not None:
+            a.k_ld = _row_ld(k, "k", dev, dt)
+            if k.shape[:2] != q.shape[:2] or k.shape[3] != q.shape[3]:
+                raise ValueError("inconsistent shapes of q and k")
+            a.H_k = k.shape[2]
+        _check(pos, "pos", dev, 3, torch.int64)
+        _check(freqs, "freqs", dev, 1, torch.float64)
+        if pos.shape[1:] != q.shape[:2]:
+            raise ValueError("pos must be [n_pos,B,S]")
+        a.rot_dim, a.n_pos = 2 * freqs.shape[0], pos.shape[0]
+        sections = [a.rot_dim // 2] if sections is None else [int(n) for n in sections]
+        if len(sections) > MAX_POS_PLANES or len(sections) != a.n_pos:
+            raise ValueError(f"sections must give the pairs of each of up to {MAX_POS_PLANES} planes")
+        for i, n in enumerate(sections):
+            a.section[i] = n
+        a.interleaved, a.inverse, a.attn_factor = int(interleaved), int(inverse), attn_factor
+        if inplace:
+            self.q_out, self.k_out = q, k
+            a.q_out_ld, a.k_out_ld = a.q_ld, a.k_ld
+        else:
+            self.q_out = _empty(q.shape, dt, dev)
+            self.k_out = None if k is None else _empty(k.shape, dt, dev)
+        a.freqs, a.pos, a.q, a.k = _ptr(freqs), _ptr(pos), _ptr(q), _ptr(k)
+        a.q_out, a.k_out = _ptr(self.q_out), _ptr(self.k_out)
+        self.inputs = (q, k, pos, freqs)
+        self.args = a
+
+    def __call__(self, stream=None):
+        _call(lib().trevs_rope, self.device, stream, ctypes.byref(self.args))
+        return self.q_out, self.k_out
+
+
+def rope(q, k, pos, stream=None, **kw):
+    """Rotary positions: returns (q_out, k_out); see Rope."""
+    return Rope(q, k, pos, **kw)(stream)
+
+
+class Kv8Cache:
+    """A paged K/V cache of n_layers layers held in 8 bits (e4m3 values, one
+    power-of-two scale for each page and KV head), empty at first:
+      k, v              uint8 [n_layers,n_pages,H_kv,page_tokens,d_head] and
+                        [n_layers,n_pages,H_kv,d_head,page_tokens]
+      k_scale, v_scale  float32 [n_layers,n_pages,H_kv]
+      table             int32 [n_slots,max_pages], the pages of each slot
+      len, ref          int32 [n_slots], tokens; [n_pages], slots that hold a page
+    """
+
+    def __init__(self, *, n_pages, page_tokens, n_slots, max_pages, H_kv, d_head, n_layers=1,
+                 device="cuda"):
+        dev = torch.device(device)
+        if dev.type == "cuda" and dev.index is None:
+            dev = torch.device("cuda", torch.cuda.current_device())
+        if min(n_pages, page_tokens, n_slots, max_pages, H_kv, d_head, n_layers) < 1:
+            raise ValueError("every size of a cache is at least 1")
+        self.device = dev
+        self.k = _empty((n_layers, n_pages, H_kv, page_tokens, d_head), torch.uint8, dev)
+        self.v = _empty((n_layers, n_pages, H_kv, d_head, page_tokens), torch.uint8, dev)
+        self.k_scale = _empty((n_layers, n_pages, H_kv), torch.float32, dev)
+        self.v_scale = _empty((n_layers, n_pages, H_kv), torch.float32, dev)
+        self.table = _empty((n_slots, max_pages), torch.int32, dev)
+        self.len = _empty((n_slots,), torch.int32, dev)
+        self.ref = _empty((n_pages,), torch.int32, dev)
+        for t in (self.k, self.v, self.k_scale, self.v_scale, self.len, self.ref):
+            t.zero_()
+        self.table.fill_(-1)
+        a = Kv8CacheArgs()
+        a.struct_size = ctypes.sizeof(Kv8CacheArgs)
+        a.n_layers, a.n_pages, a.page_tokens, a.H_kv = n_layers, n_pages, page_tokens, H_kv
+        a.d_head, a.n_slots, a.max_pages = d_head, n_slots, max_pages
+        a.k, a.v, a.k_scale, a.v_scale = _ptr(self.k), _ptr(self.v), _ptr(self.k_scale), _ptr(self.v_scale)
+        a.table, a.len, a.ref = _ptr(self.table), _ptr(self.len), _ptr(self.ref)
+        self.args = a
+
+
+class PagesReserve:
+    """Room for n_new[i] more tokens in slots[i] (None: slot i): call() returns
+    (granted, copy_src, copy_dst), int32 [n] on the device: n_new[i], or 0 where
+    the pages did not suffice, and the shared page that Kv8Copy has to copy to
+    the slot's own before rows are written, or -1."""
+
+    def __init__(self, cache, n_new, slots=None):
+        dev = cache.device
+        _check(n_new, "n_new", dev, 1, torch.int32)
+        n = n_new.shape[0]
+        _check_list(slots, "slots", dev, n)
+        self.cache, self.inputs, self.n = cache, (n_new, slots), n
+        self.granted, self.copy_src, self.copy_dst = [_empty((n,), torch.int32, dev) for _ in range(3)]
+
+    def __call__(self, stream=None):
+        n_new, slots = self.inputs
+        _call(lib().trevs_pages_reserve, self.cache.device, stream, ctypes.byref(self.cache.args), self.n,
+              _ptr(slots), _ptr(n_new), _ptr(self.granted), _ptr(self.copy_src), _ptr(self.copy_dst))
+        return self.granted, self.copy_src, self.copy_dst
+
+
+def pages_reserve(cache, n_new, slots=None, stream=None):
+    """Room for more tokens: returns (granted, copy_src, copy_dst); see PagesReserve."""
+    return PagesReserve(cache, n_new, slots)(stream)
+
+
+class PagesFork:
+    """Slot dst[i], empty before, shares the pages of the first n_tokens[i]
+    tokens of slot src[i] (None: of all): call() returns done int32 [n], 1 or,
+    where the request did nothing, 0."""
+
+    def __init__(self, cache, src, dst, n_tokens=None):
+        dev = cache.device
+        _check(src, "src", dev, 1, torch.int32)
+        n = src.shape[0]
+        _check(dst, "dst", dev, 1, torch.int32)
+        _check_list(dst, "dst", dev, n)
+        _check_list(n_tokens, "n_tokens", dev, n)
+        self.cache, self.inputs, self.n = cache, (src, dst, n_tokens), n
+        self.done = _empty((n,), torch.int32, dev)
+
+    def __call__(self, stream=None):
+        src, dst, n_tokens = self.inputs
+        _call(lib().trevs_pages_fork, self.cache.device, stream, ctypes.byref(self.cache.args), self.n,
+              _ptr(src), _ptr(dst), _ptr(n_tokens), _ptr(self.done))
+        return self.done
+
+
+def pages_fork(cache, src, dst, n_tokens=None, stream=None):
+    """Sequences that share another's pages: returns done; see PagesFork."""
+    return PagesFork(cache, src, dst, n_tokens)(stream)
+
+
+class PagesFree:
+    """slots[i] (int32, device) keeps its first keep[i] tokens (None: none) and
+    gives up its other pages."""
+
+    def __init__(self, cache, slots, keep=None):
+        _check(slots, "slots", cache.device, 1, torch.int32)
+        _check_list(keep, "keep", cache.device, slots.shape[0])
+        self.cache, self.inputs = cache, (slots, keep)
+
+    def __call__(self, stream=None):
+        slots, keep = self.inputs
+        _call(lib().trevs_pages_free, self.cache.device, stream, ctypes.byref(self.cache.args),
+              slots.shape[0], _ptr(slots), _ptr(keep))
+
+
+def pages_free(cache, slots, keep=None, stream=None):
+    """Pages given up; see PagesFree."""
+    PagesFree(cache, slots, keep)(stream)
+
+
+class Kv8Copy:
+    """Pages src[i] copied to dst[i] in every layer; pairs with -1 are skipped."""
+
+    def __init__(self, cache, src, dst):
+        _check(src, "src", cache.device, 1, torch.int32)
+        _check(dst, "dst", cache.device, 1, torch.int32)
+        _check_list(dst, "dst", cache.device, src.shape[0])
+        self.cache, self.inputs = cache, (src, dst)
+
+    def __call__(self, stream=None):
+        src, dst = self.inputs
+        _call(lib().trevs_kv8_copy_pages, self.cache.device, stream, ctypes.byref(self.cache.args),
+              src.shape[0], _ptr(src), _ptr(dst))
+
+
+def kv8_copy(cache, src, dst, stream=None):
+    """Pages copied in every layer; see Kv8Copy."""
+    Kv8Copy(cache, src, dst)(stream)
+
+
+class Kv8Write:
+    """Key and value rows k, v [B,T,H_kv,d] (fp32 or bf16) written as the last
+    n_new[b] tokens (None: T) of slots[b] (None: slot b) in one layer, their
+    room reserved before."""
+
+    def __init__(self, cache, k, v, n_new=None, slots=None, *, layer=0):
+        dev, dt = cache.device, k.dtype
+        a = Kv8WriteArgs()
+        a.struct_size = ctypes.sizeof(Kv8WriteArgs)
+        a.dtype = _dtype_code(k)
+        a.k_ld, a.v_ld = _row_ld(k, "k", dev, dt), _row_ld(v, "v", dev, dt)
+        if v.shape != k.shape or k.shape[2:] != (cache.args.H_kv, cache.args.d_head):
+            raise ValueError("k and v must be [B,T,H_kv,d_head] of the cache")
+        a.B, a.T_max, a.layer = k.shape[0], k.shape[1], layer
+        _check_list(n_new, "n_new", dev, a.B)
+        _check_list(slots, "slots", dev, a.B)
+        a.k, a.v, a.n_new, a.slots = _ptr(k), _ptr(v), _ptr(n_new), _ptr(slots)
+        self.cache, self.inputs, self.args = cache, (k, v, n_new, slots), a
+
+    def __call__(self, stream=None):
+        _call(lib().trevs_kv8_write, self.cache.device, stream, ctypes.byref(self.cache.args),
+              ctypes.byref(self.args))
+
+
+def kv8_write(cache, k, v, n_new=None, slots=None, stream=None, **kw):
+    """Rows written to the cache; see Kv8Write."""
+    Kv8Write(cache, k, v, n_new, slots, **kw)(stream)
+
+
+class Kv8Attention:
+    """Attention of query rows q [B,T,H_q,d] over one layer of the cache: the
+    first q_len[b] rows (None: T) of slots[b] (None: slot b), with causal=True
+    as the sequence's last ones, else over all its tokens.  kv_max bounds the
+    lengths of the call (0: what the cache can hold).  Output, workspace and,
+    with want_lse, the log-sum-exp of the logits [B,H_q,T] are allocated once;
+    call() enqueues and returns the output [B,T,H_q,d].  Rows past q_len[b] are
+    not written."""
+
+    def __init__(self, cache, q, q_len=None, slots=None, *, layer=0, causal=True, scale=None, kv_max=0,
+                 want_lse=False):
+        dev, dt = cache.device, q.dtype
+        a = Kv8AttentionArgs()
+        a.struct_size = ctypes.sizeof(Kv8AttentionArgs)
+        a.dtype = _dtype_code(q)
+        a.q_ld = _row_ld(q, "q", dev, dt)
+        if q.shape[3] != cache.args.d_head:
+            raise ValueError("q must be [B,T,H_q,d_head] of the cache")
+        a.B, a.T_max, a.H_q, _ = q.shape
+        _check_list(q_len, "q_len", dev, a.B)
+        _check_list(slots, "slots", dev, a.B)
+        a.layer, a.causal, a.kv_max = layer, int(causal), kv_max
+        a.scale = float(scale) if scale is not None else q.shape[3] ** -0.5
+        self.out = _empty(q.shape, dt, dev)
+        self.lse = _empty((a.B, a.H_q, a.T_max), torch.float32, dev) if want_lse else None
+        a.q, a.q_len, a.slots = _ptr(q), _ptr(q_len), _ptr(slots)
+        a.out, a.lse = _ptr(self.out), _ptr(self.lse)
+        self.cache, self.inputs, self.args = cache, (q, q_len, slots), a
+        ws = lib().trevs_kv8_attention_workspace_size(ctypes.byref(cache.args), ctypes.byref(a))
+        if ws == 0:
+            st = lib().trevs_kv8_attention(ctypes.byref(cache.args), ctypes.byref(a), None, 0, None)
+            raise TrevsError(st, "trevs_kv8_attention")
+        self.workspace = _empty((ws,), torch.uint8, dev)
+
+    def __call__(self, stream=None):
+        _call(lib().trevs_kv8_attention, self.cache.device, stream, ctypes.byref(self.cache.args),
+              ctypes.byref(self.args), self.workspace.data_ptr(), self.workspace.numel())
+        return self.out
+
+
+def kv8_attention(cache, q, q_len=None, slots=None, stream=None, **kw):
+    """Attention over the cache: returns out, or (out, lse) with want_lse=True;
+    see Kv8Attention."""
+    call = Kv8Attention(cache, q, q_len, slots, **kw)
+    out = call(stream)
+    return (out, call.lse) if kw.get("want_lse") else out
+
+
+class Kv8Compact:
+    """Stage 2's compaction inside the cache, in every layer: rows [0,P) ++
+    (P + kept_idx[b]) ++ [P+K_in, len) of slot src_slots[b] become the tokens of
+    slot dst_slots[b], whose room is reserved before."""
+
+    def __init__(self, cache, kept_idx, src_slots, dst_slots, *, P, K_in):
+        dev = cache.device
+        _check(kept_idx, "kept_idx", dev, 2, torch.int32)
+        for t, name in ((src_slots, "src_slots"), (dst_slots, "dst_slots")):
+            _check(t, name, dev, 1, torch.int32)
+            _check_list(t, name, dev, kept_idx.shape[0])
+        a = Kv8CompactArgs()
+        a.struct_size = ctypes.sizeof(Kv8CompactArgs)
+        a.B, a.n_kept = kept_idx.shape
+        a.P, a.K_in = P, K_in
+        a.kept_idx, a.src_slots, a.dst_slots = _ptr(kept_idx), _ptr(src_slots), _ptr(dst_slots)
+        self.cache, self.inputs, self.args = cache, (kept_idx, src_slots, dst_slots), a
+
+    def __call__(self, stream=None):
+        _call(lib().trevs_kv8_compact, self.cache.device, stream, ctypes.byref(self.cache.args),
+              ctypes.byref(self.args))
+
+
+def kv8_compact(cache, kept_idx, src_slots, dst_slots, stream=None, **kw):
+    """Kept rows of cached sequences moved together; see Kv8Compact."""
+    Kv8Compact(cache, kept_idx, src_slots, dst_slots, **kw)(stream)
 
 
 # ---------------------------------------------------------------- HIP events

@@ -1,0 +1,644 @@
+"""The serving cache on the GPU against its float64 oracle: rotary positions,
+rows written to the 8-bit paged cache, the attention over it, its page
+operations and compaction, and a run of them together."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as co
+from paper_2609_37581_amd import trevs
+
+pytestmark = pytest.mark.gpu
+
+TABLE = co.e4m3_bytes()
+NUMS, BYTES = zip(*sorted((v, b) for b, v in enumerate(TABLE) if np.isfinite(v) and b != 128))
+NUMS, BYTES = np.array(NUMS), np.array(BYTES, np.uint8)
+
+
+def dev(x, dtype=torch.int32):
+    return torch.tensor(np.asarray(x), dtype=dtype, device="cuda")
+
+
+def host(t):
+    return t.detach().cpu().double().numpy()
+
+
+def storage(x, dtype):
+    """float64 -> device tensor of the dtype, and the values it holds."""
+    t = torch.from_numpy(np.asarray(x, np.float64)).float().to(dtype)
+    return t.cuda(), t.double().numpy()
+
+
+def device_cache(m):
+    """The device's cache with the contents of a model."""
+    L, n, H, page, d = m.k.shape
+    c = trevs.Kv8Cache(n_pages=n, page_tokens=page, n_slots=m.n_slots, max_pages=m.max_pages, H_kv=H, d_head=d,
+                       n_layers=L)
+    enc = lambda x: torch.from_numpy(BYTES[np.searchsorted(NUMS, x)])  # noqa: E731
+    c.k.copy_(enc(m.k))
+    c.v.copy_(enc(m.v.swapaxes(3, 4)))
+    c.k_scale.copy_(torch.from_numpy(m.k_scale).float())
+    c.v_scale.copy_(torch.from_numpy(m.v_scale).float())
+    put_table(c, m)
+    return c
+
+
+def put_table(c, m):
+    c.table.copy_(dev(m.table))
+    c.len.copy_(dev(m.len))
+    c.ref.copy_(dev(m.ref))
+
+
+def check_table(c, m):
+    torch.cuda.synchronize()
+    assert c.len.tolist() == m.len
+    assert c.ref.tolist() == m.ref
+    for s in range(m.n_slots):
+        n = -(-min(max(m.len[s], 0), m.max_pages * m.page) // m.page)
+        assert c.table[s].tolist()[:n] == m.table[s][:n], s
+
+
+def check_contents(c, m):
+    """Every block of the cache, bit for bit (signed zeros aside)."""
+    torch.cuda.synchronize()
+    assert np.array_equal(host(c.k_scale), m.k_scale) and np.array_equal(host(c.v_scale), m.v_scale)
+    assert np.array_equal(TABLE[c.k.cpu().numpy()], m.k)
+    assert np.array_equal(TABLE[c.v.cpu().numpy()].swapaxes(3, 4), m.v)
+
+
+def model(rng, lens, page, H, d, n_layers=1, spare=3, slots=None, max_pages=None):
+    """A model whose sequences have these lengths, every block filled, pages in no order."""
+    need = [-(-n // page) for n in lens]
+    m = co.CacheModel(sum(need) + spare, page, slots or len(lens), max_pages or max(need + [1]), H, d, n_layers)
+    order = rng.permutation(sum(need) + spare).tolist()
+    for s, n in enumerate(need):
+        m.table[s][:n] = [order.pop() for _ in range(n)]
+        m.len[s] = lens[s]
+        for p in m.table[s][:n]:
+            m.ref[p] = 1
+    for data, scale in ((m.k, "k_scale"), (m.v, "v_scale")):
+        x = rng.normal(size=data.shape) * np.exp2(rng.integers(-2, 3, data.shape[:3]))[..., None, None]
+        sc = co.block_scale(np.abs(x).max((3, 4)))
+        data[:] = co.e4m3(x / sc[..., None, None])
+        setattr(m, scale, sc)
+    return m
+
+
+# ------------------------------------------------------------------- rotary
+ROPE = [  # B, S, H_q, H_k, d, rot, sections, far
+    (1, 1, 1, 0, 64, 16, [8], 100), (2, 3, 7, 1, 128, 128, [16, 24, 24], 4096), (3, 37, 4, 4, 64, 48, [0, 24], 70000),
+    (1, 300, 28, 4, 128, 64, [32], 1 << 20), (2, 5, 3, 2, 256, 256, [128], 1 << 33), (5, 1, 32, 8, 128, 128, [1, 2, 60, 1], 999),
+    (1, 1100, 2, 2, 128, 96, [48], 32768),
+]
+
+
+@pytest.mark.parametrize("shape", ROPE)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("inter", [False, True])
+def test_rope(shape, dtype, inter):
+    B, S, H_q, H_k, d, rot, sections, far = shape
+    print(f"[rope] {shape} {dtype} {inter}", flush=True)
+    rng = np.random.default_rng(B * 7 + S)
+    pos = rng.integers(0, far, (len(sections), B, S))
+    f = co.rope_frequencies(rot, base=500.0)
+    fd, pd = dev(f, torch.float64), dev(pos, torch.int64)
+    # q and k as slices of a fused projection with values behind them
+    H = H_q + 2 * H_k
+    fused, x = storage(rng.normal(size=(B, S, H, d)), dtype)
+    q, k = fused[:, :, :H_q], fused[:, :, H_q:H_q + H_k] if H_k else None
+    before = fused.clone()
+    for inverse in (False, True):
+        call = trevs.Rope(q, k, pd, freqs=fd, sections=sections, interleaved=inter, inverse=inverse, attn_factor=1.25)
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(fused, before)
+        # per pair: the angle is off by 2 pi 2^-25 (its fraction cast to 32 bits), sine, cosine, their
+        # factor, two products and a sum by 2^-24 each and two ulps for the functions
+        size = co.rope(np.abs(x), np.zeros_like(pos), f, sections, inter) * 0
+        first = np.arange(rot // 2) * (2 if inter else 1)
+        second = first + (1 if inter else rot // 2)
+        pair = np.abs(x[..., first]) + np.abs(x[..., second])
+        size[..., first] = size[..., second] = 1.25 * pair
+        want = co.rope(x, pos, f, sections, inter, inverse, 1.25)
+        # the oracle forms pos * f in 64 bits: at 2^33 positions and f <= 1/2pi the product is up to
+        # 1.4e9 turns, rounded by 2^-53 of that = 1.5e-7 turns = 9.5e-7 radians
+        turns = far * f.max() * 2.0 ** -53
+        tol = size * (2 * math.pi * (2.0 ** -25 + turns) + 8 * 2.0 ** -24)
+        tol = tol + (np.abs(want) + tol) * torch.finfo(dtype).eps / 2 * (dtype == torch.bfloat16)
+        assert np.all(np.abs(host(call.q_out) - want[:, :, :H_q]) <= tol[:, :, :H_q])
+        assert torch.equal(call.q_out[..., rot:], q[..., rot:])
+        if H_k:
+            assert np.all(np.abs(host(call.k_out) - want[:, :, H_q:H_q + H_k]) <= tol[:, :, H_q:H_q + H_k])
+        # in place, the same bits, and nothing else of the buffer changes
+        trevs.rope(q, k, pd, freqs=fd, sections=sections, interleaved=inter, inverse=inverse, attn_factor=1.25,
+                   inplace=True)
+        torch.cuda.synchronize()
+        assert torch.equal(q, call.q_out) and (not H_k or torch.equal(k, call.k_out))
+        assert torch.equal(fused[:, :, H_q + H_k:], before[:, :, H_q + H_k:])
+        fused.copy_(before)
+
+
+def test_rope_inverse_is_the_gradient():
+    """The rotation is linear: its gradient against differences of its own
+    outputs along each direction, and <rope(x), y> = <x, inverse(y)>."""
+    rng = np.random.default_rng(0)
+    x, xs = storage(rng.normal(size=(1, 9, 2, 64)), torch.float32)
+    y, ys = storage(rng.normal(size=(1, 9, 2, 64)), torch.float32)
+    pos, f = dev(rng.integers(0, 5000, (1, 1, 9)), torch.int64), dev(co.rope_frequencies(48), torch.float64)
+    out, _ = trevs.rope(x, None, pos, freqs=f, attn_factor=0.75)
+    grad, _ = trevs.rope(y, None, pos, freqs=f, attn_factor=0.75, inverse=True)
+    a, b = (host(out) * ys).sum(), (xs * host(grad)).sum()
+    bound = 16 * 2.0 ** -24 * (np.abs(xs).sum() * np.abs(ys).max() * 2)
+    assert abs(a - b) <= bound
+    step, ss = storage(rng.normal(size=(1, 9, 2, 64)), torch.float32)
+    moved, _ = trevs.rope(x + step, None, pos, freqs=f, attn_factor=0.75)
+    diff = (host(moved) - host(out)) * ys
+    bound = 16 * 2.0 ** -24 * (np.abs(xs) + np.abs(ss) + 8).sum() * np.abs(ys).max() * 2
+    assert abs(diff.sum() - (ss * host(grad)).sum()) <= bound
+
+
+# -------------------------------------------------------------------- write
+@pytest.mark.parametrize("page", [16, 32, 64])
+@pytest.mark.parametrize("H,d", [(1, 64), (3, 128), (2, 256)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_write(page, H, d, dtype):
+    print(f"[write] {page} {H} {d} {dtype}", flush=True)
+    rng = np.random.default_rng(page + d)
+    lens = [1, page, page + 1, 3 * page - 1, 0, 2 * page + 7, 5, 4 * page]
+    n_new = [1, 3, 1, 2 * page + 5, 2, 500, 0, 2 * page]  # 500 is cut to the length and to T
+    slots = [3, 0, 6, 2, 4, 1, 5, 7]
+    m = model(rng, lens, page, H, d, n_layers=2, max_pages=5)
+    m.table[7][1] = -1           # a page that is not there, one that cannot be
+    m.table[5][2] = m.n_pages
+    T = 2 * page + 9
+    fused, x = storage(rng.normal(size=(8, T, 2 * H + 1, d)) * np.exp2(rng.integers(-3, 4, (8, T, 1, 1))), dtype)
+    n_new = [n_new[s] for s in slots]
+    c = device_cache(m)
+    trevs.kv8_write(c, fused[:, :, :H], fused[:, :, H:2 * H], dev(n_new), dev(slots), layer=1)
+    m.write(x[:, :, :H], x[:, :, H:2 * H], n_new, slots, layer=1)
+    check_contents(c, m)
+    check_table(c, m)
+
+
+def test_write_scales_at_their_ends():
+    """Zero blocks, values next to a scale's border, the largest and the smallest floats."""
+    m = model(np.random.default_rng(1), [16] * 8, 16, 1, 64)
+    x = np.zeros((8, 16, 1, 64))
+    for b, top in enumerate([0.0, 448.0, np.nextafter(np.float32(448), np.float32(1000)), 1.75 * 2.0 ** 5, 3.4e38,
+                             2.0 ** -149, 2.0 ** -118, 1e-30]):
+        x[b, 3] = top * np.linspace(-1, 1, 64)
+    k, kv = storage(x, torch.float32)
+    c = device_cache(m)
+    trevs.kv8_write(c, k, -k)
+    m.write(kv, -kv)
+    check_contents(c, m)
+
+
+def test_write_token_by_token_raises_scales():
+    rng = np.random.default_rng(2)
+    m = model(rng, [0, 0, 0], 32, 2, 128, spare=8, max_pages=2)
+    c = device_cache(m)
+    for t in range(40):
+        n = [1, int(t % 3 == 0), 1]
+        g = trevs.pages_reserve(c, dev(n))[0]
+        assert g.tolist() == m.reserve(n)[0]
+        k, kv = storage(rng.normal(size=(3, 1, 2, 128)) * 2.0 ** (t // 4 % 9), torch.bfloat16)
+        v, vv = storage(rng.normal(size=(3, 1, 2, 128)) * 2.0 ** (7 - t % 8), torch.bfloat16)
+        trevs.kv8_write(c, k, v, g)
+        m.write(kv, vv, n)
+    check_contents(c, m)
+    check_table(c, m)
+
+
+# ---------------------------------------------------------------- attention
+def check_attention(m, c, qs, out, lse, dtype, **kw):
+    want, want_lse, weight, size = m.attention(qs, **kw)
+    n = max(m.len) + 64
+    d = qs.shape[3]
+    # logits: fp32 sums of d exact products (bf16 parts times e4m3 numbers) and a few roundings of
+    # their result; a logit's error is relative in its weight, for numerator and denominator
+    logit = (d + 8) * 2.0 ** -24 * size
+    # weights rounded to bf16 for the products (fp32: three parts, 2^-24), exp2 and sums over n keys
+    w = (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -22) + (n + 16) * 2.0 ** -24
+    rows = np.isfinite(want)
+    got = host(out)
+    tol = (2 * logit.transpose(0, 2, 1)[..., None] + w) * weight
+    tol = tol + (np.abs(want) + tol) * (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -22)
+    err = np.abs(got - want)
+    assert np.all(err[rows] <= tol[rows]), (np.nanmax(err), np.nanmax(np.where(rows, err - tol, -1)))
+    assert np.all(got[~rows] == 7.0)  # rows past q_len keep what they held
+    if lse is not None:
+        gl = host(lse)
+        some = np.isfinite(want_lse)
+        empty = np.isneginf(want_lse)
+        assert np.array_equal(np.isneginf(gl), empty)
+        tl = logit + (n + 16) * 2.0 ** -24 + 2.0 ** -22 * np.abs(np.where(some, want_lse, 0))
+        assert np.all(np.abs(gl[some] - want_lse[some]) <= tl[some])
+        assert np.all(gl[np.isnan(want_lse)] == 7.0)
+
+
+def run_attention(m, c, q, qs, dtype, q_len=None, slots=None, **kw):
+    call = trevs.Kv8Attention(c, q, None if q_len is None else dev(q_len), None if slots is None else dev(slots),
+                              want_lse=True, **kw)
+    call.out.fill_(7.0)
+    call.lse.fill_(7.0)
+    call()
+    torch.cuda.synchronize()
+    check_attention(m, c, qs, call.out, call.lse, dtype, q_len=q_len, slots=slots, **kw)
+    return call
+
+
+ATTN = [  # page, H_q, H_kv, d, T, lens
+    (16, 4, 4, 64, 1, [1, 16, 17, 0, 333]), (64, 7, 1, 128, 1, [64, 63, 65, 1, 1000]),
+    (32, 28, 4, 128, 1, [700, 31, 32]), (16, 40, 2, 128, 1, [100, 257]), (64, 8, 1, 256, 1, [129, 5]),
+    (32, 6, 2, 64, 5, [3, 40, 0, 5]), (16, 28, 4, 128, 3, [200, 3, 19]), (64, 28, 4, 128, 33, [64, 33, 500]),
+    (32, 4, 4, 128, 70, [70, 200, 129]), (64, 2, 2, 256, 45, [45, 300]), (16, 3, 1, 64, 130, [131, 100]),
+    (64, 16, 2, 64, 17, [400]), (32, 8, 1, 256, 40, [90]), (16, 33, 1, 64, 1, [77, 15]), (64, 1, 1, 128, 150, [150]),
+]
+
+
+@pytest.mark.parametrize("shape", ATTN)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention(shape, dtype, causal):
+    page, H_q, H_kv, d, T, lens = shape
+    print(f"[attn] {shape} {dtype} {causal}", flush=True)
+    rng = np.random.default_rng(sum(lens) + d)
+    m = model(rng, lens, page, H_kv, d)
+    c = device_cache(m)
+    fused, x = storage(rng.normal(size=(len(lens), T, H_q + 3, d)), dtype)
+    q, qs = fused[:, :, :H_q], x[:, :, :H_q]
+    q_len = [max(0, T - 2 * b) for b in range(len(lens))]
+    run_attention(m, c, q, qs, dtype, q_len=q_len, causal=causal)
+    run_attention(m, c, q, qs, dtype, causal=causal, kv_max=max(lens), scale=0.31)
+
+
+@pytest.mark.parametrize("T", [1, 40])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_attention_masked_places_hold_anything(T, dtype):
+    """NaN bytes behind the last token, in pages of no sequence and in unused
+    scales; absent pages; lengths past the table; a slot out of range; lengths cut by kv_max."""
+    print(f"[attn masked] {T} {dtype}", flush=True)
+    rng = np.random.default_rng(5)
+    m = model(rng, [150, 37, 260, 64, 90], 32, 2, 128, spare=6)
+    m.table[0][1] = -5
+    m.table[2][0], m.table[2][8] = m.n_pages + 3, -1
+    m.table[3] = [-1] * m.max_pages  # every page absent: the row is empty
+    c = device_cache(m)
+    used = set()
+    for s in range(5):
+        for j in range(-(-m.len[s] // 32)):
+            p, n = m.table[s][j], min(32, m.len[s] - 32 * j)
+            if 0 <= p < m.n_pages:
+                used.add(p)
+                c.k[0, p, :, n:] = 0x7f
+                c.v[0, p, :, :, n:] = 0xff
+    for p in set(range(m.n_pages)) - used:
+        c.k[0, p], c.v[0, p] = 0xff, 0x7f
+        c.k_scale[0, p], c.v_scale[0, p] = math.nan, math.inf
+    q, qs = storage(rng.normal(size=(5, T, 4, 128)), dtype)
+    for causal in (True, False):
+        run_attention(m, c, q, qs, dtype, causal=causal)
+        run_attention(m, c, q, qs, dtype, causal=causal, slots=[4, 2, 0, 3, 99], kv_max=100)
+    m.len[1], m.len[4] = 100000, -3
+    c = device_cache(m)  # (the bytes behind sequence 1 are its tokens now: numbers again)
+    m.len[1], m.len[4] = m.max_pages * 32, 0
+    run_attention(m, c, q, qs, dtype)
+
+
+def test_attention_large_logits_and_infinite_neighbours():
+    """Logits of +-1e4: the running maximum keeps every weight finite."""
+    rng = np.random.default_rng(6)
+    m = model(rng, [300, 65], 16, 1, 64)
+    m.k_scale *= 2.0 ** 9
+    c = device_cache(m)
+    for dtype in (torch.float32, torch.bfloat16):
+        q, qs = storage(rng.normal(size=(2, 20, 2, 64)) * 30, dtype)
+        call = trevs.Kv8Attention(c, q)
+        call.out.fill_(7.0)
+        call()
+        torch.cuda.synchronize()
+        assert torch.isfinite(call.out).all()
+        check_attention(m, c, qs, call.out, None, dtype)
+
+
+@pytest.mark.parametrize("T", [1, 24])
+def test_attention_long_and_layers(T):
+    """Long sequences beside short ones, in the second of two layers; the
+    same call twice gives the same bits."""
+    print(f"[attn long] {T}", flush=True)
+    rng = np.random.default_rng(7)
+    m = model(rng, [3000, 40, 1111], 64, 1, 64, n_layers=2)
+    c = device_cache(m)
+    q, qs = storage(rng.normal(size=(3, T, 2, 64)), torch.bfloat16)
+    first = run_attention(m, c, q, qs, torch.bfloat16, layer=1).out.clone()
+    again = run_attention(m, c, q, qs, torch.bfloat16, layer=1).out
+    assert torch.equal(first, again)
+
+
+def test_offsets_past_32_bits():
+    """Pages whose bytes lie past 4 GiB: written, read, copied and compacted."""
+    page, H, d, n_pages = 64, 32, 256, 8300  # 512 KiB a page and side, 4.3 GB
+    c = trevs.Kv8Cache(n_pages=n_pages, page_tokens=page, n_slots=3, max_pages=3, H_kv=H, d_head=d)
+    top = n_pages - 1
+    m = co.CacheModel(8, page, 3, 3, H, d)
+    m.table, m.len, m.ref = [[7, 0, 6], [5, 4, -1], [-1] * 3], [150, 100, 0], [1, 0, 0, 0, 1, 1, 1, 1]
+    far = lambda p: p if p < 4 else top - (7 - p)  # noqa: E731  model page -> device page
+    c.table.copy_(dev([[far(p) if p >= 0 else -1 for p in row] for row in m.table]))
+    c.len.copy_(dev(m.len))
+    rng = np.random.default_rng(8)
+    k, ks = storage(rng.normal(size=(2, 150, H, d)), torch.bfloat16)
+    trevs.kv8_write(c, k, -k, dev([150, 100]))
+    m.write(ks, -ks, [150, 100])
+    kept = [[1, 5, 6, 40]]
+    trevs.kv8_compact(c, dev(kept), dev([0]), dev([1]), P=20, K_in=100)
+    m.compact(kept, [0], [1], 20, 100)
+    trevs.kv8_copy(c, dev([top, top - 2]), dev([1, top - 4]))
+    m.copy([7, 5], [1, 3])
+    torch.cuda.synchronize()
+    for p in (0, 1, 3, 4, 5, 6, 7):
+        at = top - 4 if p == 3 else far(p)
+        assert np.array_equal(TABLE[c.k[0, at].cpu().numpy()], m.k[0, p]), p
+        assert np.array_equal(TABLE[c.v[0, at].cpu().numpy()].swapaxes(1, 2), m.v[0, p]), p
+        assert np.array_equal(host(c.k_scale[0, at]), m.k_scale[0, p])
+    q, qs = storage(rng.normal(size=(2, 1, H, d)), torch.bfloat16)
+    run_attention(m, c, q, qs, torch.bfloat16)
+
+
+# -------------------------------------------------------------------- pages
+@pytest.mark.parametrize("seed", range(4))
+def test_page_operations_in_any_order(seed):
+    """Random requests with repeated and invalid slots, and shortages."""
+    print(f"[pages] {seed}", flush=True)
+    rng = np.random.default_rng(seed)
+    page = [16, 32, 64, 16][seed]
+    n_pages, n_slots, most = [(40, 12, 8), (23, 6, 9), (9000, 40, 300), (64, 64, 4)][seed]
+    m = co.CacheModel(n_pages, page, n_slots, most, 1, 64)
+    c = device_cache(m)
+    for step in range(120):
+        n = int(rng.integers(1, 2 * n_slots))
+        slots = rng.integers(-1, n_slots + 1, n).tolist()
+        op = rng.integers(4)
+        if op == 0 or op == 3:
+            new = rng.integers(-1, most * page // 2, n).tolist()
+            if step % 5 == 0:  # one request a slot, in slot order
+                n, slots = n_slots, None
+                new = rng.integers(0, most * page // 4, n).tolist()
+            got = trevs.pages_reserve(c, dev(new), None if slots is None else dev(slots))
+            assert [t.tolist() for t in got] == [list(x) for x in m.reserve(new, slots)]
+        elif op == 1:
+            src = rng.integers(-1, n_slots + 1, n).tolist()
+            tokens = None if rng.random() < 0.5 else rng.integers(-5, most * page + 5, n).tolist()
+            done = trevs.pages_fork(c, dev(src), dev(slots), None if tokens is None else dev(tokens))
+            assert done.tolist() == m.fork(src, slots, tokens)
+        else:
+            keep = None if rng.random() < 0.5 else rng.integers(-5, most * page, n).tolist()
+            trevs.pages_free(c, dev(slots), None if keep is None else dev(keep))
+            m.free(slots, keep)
+        check_table(c, m)
+
+
+@pytest.mark.parametrize("n", [1, 1024])
+def test_reserve_many_requests(n):
+    """The most requests of a call, all ending in one shared page; short of pages by a few."""
+    for spare in (0, 1, n // 2, 2 * n):
+        m = co.CacheModel(3 + spare, 16, n + 1, 4, 1, 64)
+        m.reserve([20])
+        m.fork([0] * n, list(range(1, n + 1)))
+        c = device_cache(m)
+        new = [1 + i % 30 for i in range(n)]
+        slots = list(range(n, 0, -1))
+        got = trevs.pages_reserve(c, dev(new), dev(slots))
+        assert [t.tolist() for t in got] == [list(x) for x in m.reserve(new, slots)]
+        check_table(c, m)
+
+
+def test_reserve_counts_that_are_not_aligned():
+    m = co.CacheModel(37, 16, 3, 12, 1, 64)
+    m.reserve([50, 20])
+    c = device_cache(m)
+    raw = torch.zeros(38, dtype=torch.int32, device="cuda")
+    c.ref = raw[1:]
+    c.ref.copy_(dev(m.ref))
+    c.args.ref = c.ref.data_ptr()
+    new = [3, 100, 190]
+    assert [t.tolist() for t in trevs.pages_reserve(c, dev(new))] == [list(x) for x in m.reserve(new)]
+    check_table(c, m)
+    assert raw[0].item() == 0
+
+
+def test_copy_pages():
+    rng = np.random.default_rng(9)
+    for page, H, d in ((16, 1, 64), (64, 5, 128)):
+        m = model(rng, [100], page, H, d, n_layers=3, spare=8)
+        c = device_cache(m)
+        src, dst = [0, -1, 3, 4, m.n_pages, 5], [1, 2, -1, 6, 7, m.n_pages]
+        trevs.kv8_copy(c, dev(src), dev(dst))
+        m.copy(src, dst)
+        check_contents(c, m)
+
+
+# ------------------------------------------------------------------ compact
+@pytest.mark.parametrize("page,H,d", [(16, 2, 64), (32, 1, 256), (64, 3, 128)])
+def test_compact(page, H, d):
+    print(f"[compact] {page} {H} {d}", flush=True)
+    rng = np.random.default_rng(page)
+    P, K_in, K = 21, 150, 40
+    lens = [P + K_in, P + K_in + 33, P + K_in + 1, P + K_in - 1, P + K_in + 90, 500]
+    outs = [n - K_in + K for n in lens]
+    outs[2] -= 10                   # less room than rows: the last are dropped
+    outs[5] += 3 * page             # more room than rows: the rest stays as it is
+    m = model(rng, lens + outs, page, H, d, n_layers=2)
+    m.table[1][3] = -1              # rows of a page that is not there are zeros
+    m.table[6 + 4][1] = m.n_pages   # and a destination page that is not there is passed over
+    c = device_cache(m)
+    kept = np.sort(np.argsort(rng.random((7, K_in)), 1)[:, :K], 1)
+    kept[4, 0], kept[4, -1] = -7, K_in + 5
+    src, dst = [0, 1, 2, 3, 4, 5, -1], [6, 7, 8, 9, 10, 11, 0]
+    trevs.kv8_compact(c, dev(kept), dev(src), dev(dst), P=P, K_in=K_in)
+    m.compact(kept, src, dst, P, K_in)
+    check_contents(c, m)
+    check_table(c, m)
+
+
+# ------------------------------------------------------------------ together
+class Serving:
+    """One image with two questions: rotary positions, stage 2, the pruned rows
+    into the cache, a fork for the second question, decode steps for both; and
+    the unpruned layer's cache compacted with stage 2's own choice."""
+
+    def __init__(self, dtype):
+        rng = np.random.default_rng(11)
+        self.B, self.P, self.K_in, self.T, self.K = 2, 19, 180, 23, 60
+        self.H_q, self.H_kv, self.d, self.page, self.steps = 8, 2, 128, 32, 6
+        B, S = self.B, self.P + self.K_in + self.T
+        self.S, self.S2 = S, S - self.K_in + self.K
+        t = lambda *s: storage(rng.normal(size=s), dtype)[0]  # noqa: E731
+        self.q, self.k, self.v, self.hidden = (t(B, S, self.H_q, self.d), t(B, S, self.H_kv, self.d),
+                                               t(B, S, self.H_kv, self.d), t(B, S, 64))
+        self.pos = dev(np.broadcast_to(np.arange(S), (3, B, S)), torch.int64)
+        self.freqs = trevs.rope_frequencies(self.d).cuda()
+        self.cache = trevs.Kv8Cache(n_pages=64, page_tokens=self.page, n_slots=8, max_pages=10, H_kv=self.H_kv,
+                                    d_head=self.d, n_layers=2)
+        kw = dict(freqs=self.freqs, sections=[16, 24, 24])
+        self.rope = trevs.Rope(self.q, self.k, self.pos, **kw)
+        self.inllm = trevs.Inllm(self.rope.q_out, self.rope.k_out, self.v, self.hidden, self.pos, P=self.P,
+                                 K_in=self.K_in, n_keep_heads=4, k_keep=self.K)
+        c = self.cache
+        # slots 0, 1: the unpruned sequences (layer 0); 2, 3: the pruned ones; 4..7: two questions on each of 2, 3
+        self.room = trevs.PagesReserve(c, dev([S, S, self.S2, self.S2]), dev([0, 1, 2, 3]))
+        self.write0 = trevs.Kv8Write(c, self.rope.k_out, self.v, slots=dev([0, 1]), layer=0)
+        self.write1 = trevs.Kv8Write(c, self.inllm.k_out, self.inllm.v_out, slots=dev([2, 3]), layer=1)
+        self.compact = trevs.Kv8Compact(c, self.inllm.kept_idx, dev([0, 1]), dev([2, 3]), P=self.P, K_in=self.K_in)
+        self.fork = trevs.PagesFork(c, dev([2, 2, 3, 3]), dev([4, 5, 6, 7]))
+        self.xq = t(self.steps, 4, 1, self.H_q, self.d)
+        self.xk, self.xv = t(self.steps, 4, 1, self.H_kv, self.d), t(self.steps, 4, 1, self.H_kv, self.d)
+        self.decode = []
+        slots = dev([4, 5, 6, 7])
+        for i in range(self.steps):
+            at = dev(np.full((3, 4, 1), S + i), torch.int64)
+            rope = trevs.Rope(self.xq[i], self.xk[i], at, **kw)
+            room = trevs.PagesReserve(c, dev([1, 1, 1, 1]), slots)
+            self.decode.append((rope, room, trevs.Kv8Copy(c, room.copy_src, room.copy_dst),
+                                [trevs.Kv8Write(c, rope.k_out, self.xv[i], room.granted, slots, layer=l) for l in (0, 1)],
+                                [trevs.Kv8Attention(c, rope.q_out, room.granted, slots, layer=l) for l in (0, 1)]))
+        self.free = trevs.PagesFree(c, dev(list(range(8))))
+        self.prompt = trevs.Kv8Attention(c, self.rope.q_out, slots=dev([0, 1]), layer=0, kv_max=S)
+
+    def __call__(self):
+        self.free()
+        self.rope()
+        self.inllm()
+        self.room()
+        self.write0()
+        self.prompt()
+        self.compact()  # layer 0: the pruned sequences from the unpruned ones (layer 1 is written below)
+        self.write1()
+        self.fork()
+        for rope, room, copy, writes, attns in self.decode:
+            rope()
+            room()
+            copy()
+            for w, a in zip(writes, attns):
+                w()
+                a()
+
+    def outputs(self):
+        return ([self.rope.q_out, self.rope.k_out, self.inllm.kept_idx, self.prompt.out]
+                + [a.out for step in self.decode for a in step[4]])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_serving_run(dtype):
+    print(f"[serving] {dtype}", flush=True)
+    s = Serving(dtype)
+    s()
+    torch.cuda.synchronize()
+    # the model, fed with the GPU's rotated rows and stage 2's choice
+    m = co.CacheModel(64, s.page, 8, 10, s.H_kv, s.d, 2)
+    m.reserve([s.S, s.S, s.S2, s.S2])
+    m.write(host(s.rope.k_out), host(s.v), slots=[0, 1], layer=0)
+    check_attention(m, s.cache, host(s.rope.q_out), s.prompt.out, None, dtype, slots=[0, 1])
+    m.compact(s.inllm.kept_idx.tolist(), [0, 1], [2, 3], s.P, s.K_in)
+    m.write(host(s.inllm.k_out), host(s.inllm.v_out), slots=[2, 3], layer=1)
+    m.fork([2, 2, 3, 3], [4, 5, 6, 7])
+    for i, (rope, room, _, writes, attns) in enumerate(s.decode):
+        granted, src, dst = m.reserve([1] * 4, [4, 5, 6, 7])
+        assert room.granted.tolist() == granted and room.copy_src.tolist() == src and room.copy_dst.tolist() == dst
+        m.copy(src, dst)
+        for layer in (0, 1):
+            m.write(host(rope.k_out), host(s.xv[i]), slots=[4, 5, 6, 7], layer=layer)
+            check_attention(m, s.cache, host(rope.q_out), attns[layer].out, None, dtype, slots=[4, 5, 6, 7],
+                            layer=layer)
+    check_table(s.cache, m)
+    live = [p for p in range(64) if m.ref[p]]
+    assert np.array_equal(host(s.cache.k_scale)[1, live], m.k_scale[1, live])
+    assert np.array_equal(TABLE[s.cache.v.cpu().numpy()].swapaxes(3, 4)[1, live], m.v[1, live])
+
+
+def test_serving_run_captured():
+    """The run captured into a graph and replayed, with the program's own eager
+    work between the replays, gives the eager run's bits; so does another stream."""
+    s = Serving(torch.bfloat16)
+    s()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in s.outputs()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for t in s.outputs():
+        t.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        s()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, s.outputs()))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        s()
+    for r in range(4):
+        for t in s.outputs():
+            t.view(torch.uint8).fill_(0x5A)
+        if r % 2:
+            s.cache.k.fill_(0x7F)
+            s.cache.v.fill_(0xFF)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, s.outputs())), r
+        s()
+        torch.cuda.synchronize()
+
+
+# ----------------------------------------------------------------- refusals
+def test_binding_refusals():
+    c = trevs.Kv8Cache(n_pages=8, page_tokens=16, n_slots=2, max_pages=4, H_kv=2, d_head=64)
+    x = torch.zeros((2, 3, 2, 64), device="cuda")
+    n = dev([1, 1])
+    with pytest.raises(TypeError):
+        trevs.kv8_write(c, x.half(), x.half())
+    with pytest.raises(TypeError):
+        trevs.kv8_write(c, x, x.bfloat16())
+    with pytest.raises(ValueError):
+        trevs.kv8_write(c, x[:, :, :1], x[:, :, :1])
+    with pytest.raises(ValueError):
+        trevs.kv8_write(c, x.transpose(1, 2).contiguous().transpose(1, 2), x)  # heads not dense
+    with pytest.raises(ValueError):
+        trevs.kv8_write(c, x, x, dev([1, 1, 1]))
+    with pytest.raises(TypeError):
+        trevs.kv8_write(c, x, x, n.long())
+    with pytest.raises(ValueError):
+        trevs.kv8_write(c, x.cpu(), x.cpu())
+    with pytest.raises(trevs.TrevsError):
+        trevs.kv8_write(c, x, x, layer=1)
+    with pytest.raises(ValueError):
+        trevs.kv8_attention(c, torch.zeros((2, 1, 2, 128), device="cuda"))
+    with pytest.raises(trevs.TrevsError):
+        trevs.kv8_attention(c, torch.zeros((2, 1, 3, 64), device="cuda"))
+    with pytest.raises(trevs.TrevsError):
+        trevs.kv8_attention(c, x, kv_max=65)
+    with pytest.raises(ValueError):
+        trevs.pages_reserve(c, n, dev([0]))
+    with pytest.raises(trevs.TrevsError):
+        trevs.pages_reserve(c, dev([1, 1, 1]))
+    with pytest.raises(TypeError):
+        trevs.pages_free(c, None)
+    with pytest.raises(ValueError):
+        trevs.pages_fork(c, n, dev([1]))
+    with pytest.raises(trevs.TrevsError):
+        trevs.kv8_compact(c, dev([[0, 1]]), dev([0]), dev([1]), P=0, K_in=1)
+    pos, f = torch.zeros((1, 2, 3), dtype=torch.int64, device="cuda"), torch.zeros(32, dtype=torch.float64, device="cuda")
+    with pytest.raises(ValueError):
+        trevs.rope(x, x[:, :2], pos, freqs=f)
+    with pytest.raises(ValueError):
+        trevs.rope(x, x, pos[:, :, :2].contiguous(), freqs=f)
+    with pytest.raises(trevs.TrevsError):
+        trevs.rope(x, x, pos, freqs=f, sections=[31])
+    with pytest.raises(ValueError):
+        trevs.rope(x, x, pos, freqs=f, sections=[16, 16])
+    with pytest.raises(TypeError):
+        trevs.rope(x, x, pos, freqs=f.float())
+    with pytest.raises(ValueError):
+        trevs.Kv8Cache(n_pages=0, page_tokens=16, n_slots=2, max_pages=4, H_kv=2, d_head=64)
