@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "../../include/trevs.h"
 #include "common.hpp"
 
@@ -150,10 +152,19 @@ struct AttnArgs {
   const int32_t* slots;
   void* out;
   float* lse;
-  int B, T_max, H_q, G, causal, kv_max;
+  int B, T_max, H_q, G, causal, kv_max, page_shift;
   float scale_log2e;
+  int row_tiles, n_split;
+  float* part;              // n_split > 1: [B,H_kv,T_max*G,n_split,D] sums not yet divided
+  float2* part_ml;          // and [B,H_kv,T_max*G,n_split] (maximum, sum), base 2
 };
-hipError_t launch_kv8_attention(const AttnArgs& a, int dtype, int d_head, int page, hipStream_t s);
+// Launch shape of one problem size.
+struct AttnPlan {
+  int rows;                 // query rows of a workgroup
+  int row_tiles, n_split;
+};
+AttnPlan attn_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtype, int d_head);
+hipError_t launch_kv8_attention(const AttnArgs& a, const AttnPlan& p, int dtype, int d_head, hipStream_t s);
 
 struct PagesArgs {
   int32_t* table;

@@ -129,6 +129,8 @@ trevs_status validate_list(const trevs_kv8_cache* c, int32_t n, const int32_t* s
   return TREVS_OK;
 }
 
+int page_shift(const trevs_kv8_cache* c) { return c->page_tokens == 16 ? 4 : c->page_tokens == 32 ? 5 : 6; }
+
 PagesArgs pages_args(const trevs_kv8_cache* c, int n) {
   PagesArgs p;
   p.table = c->table;
@@ -137,7 +139,7 @@ PagesArgs pages_args(const trevs_kv8_cache* c, int n) {
   p.n_pages = c->n_pages;
   p.n_slots = c->n_slots;
   p.max_pages = c->max_pages;
-  p.page_shift = c->page_tokens == 16 ? 4 : c->page_tokens == 32 ? 5 : 6;
+  p.page_shift = page_shift(c);
   p.n = n;
   return p;
 }
@@ -185,6 +187,24 @@ trevs_status validate_attention(const trevs_kv8_cache* c, const trevs_kv8_attent
   for (const Span& o : out)
     if (meets_cache(c, o)) return TREVS_ERR_INVALID_ARG;
   return TREVS_OK;
+}
+
+int max_keys(const trevs_kv8_cache* c, const trevs_kv8_attention_args* a) {
+  return a->kv_max ? a->kv_max : c->max_pages * c->page_tokens;
+}
+
+// Parts of split rows: (maximum, sum) pairs, then the sums of values.
+struct AttnLayout {
+  AttnPlan plan;
+  size_t part, total;
+};
+AttnLayout attention_layout(const trevs_kv8_cache* c, const trevs_kv8_attention_args* a) {
+  AttnLayout L;
+  L.plan = attn_plan(a->B, a->T_max, c->H_kv, a->H_q / c->H_kv, max_keys(c, a), a->dtype, c->d_head);
+  const size_t parts = L.plan.n_split > 1 ? (size_t)a->B * a->T_max * a->H_q * L.plan.n_split : 0;
+  L.part = align_up(parts * sizeof(float2));
+  L.total = std::max(L.part + align_up(parts * c->d_head * sizeof(float)), kWsAlign);
+  return L;
 }
 
 trevs_status validate_compact(const trevs_kv8_cache* c, const trevs_kv8_compact_args* a) {
@@ -348,14 +368,15 @@ trevs_status trevs_kv8_write(const trevs_kv8_cache* c, const trevs_kv8_write_arg
 
 size_t trevs_kv8_attention_workspace_size(const trevs_kv8_cache* c, const trevs_kv8_attention_args* a) {
   if (validate_attention(c, a) != TREVS_OK) return 0;
-  return kWsAlign;
+  return attention_layout(c, a).total;
 }
 
 trevs_status trevs_kv8_attention(const trevs_kv8_cache* c, const trevs_kv8_attention_args* a, void* ws,
                                  size_t ws_bytes, void* stream) {
   TREVS_TRY(validate_attention(c, a));
-  TREVS_TRY(check_ws(ws, ws_bytes, kWsAlign));
-  AttnArgs t;
+  const AttnLayout L = attention_layout(c, a);
+  TREVS_TRY(check_ws(ws, ws_bytes, L.total));
+  AttnArgs t = {};
   t.c = layer_view(*c, a->layer);
   t.q = a->q;
   t.q_ld = a->q_ld ? a->q_ld : (int64_t)a->H_q * c->d_head;
@@ -368,9 +389,12 @@ trevs_status trevs_kv8_attention(const trevs_kv8_cache* c, const trevs_kv8_atten
   t.H_q = a->H_q;
   t.G = a->H_q / c->H_kv;
   t.causal = a->causal;
-  t.kv_max = a->kv_max ? a->kv_max : c->max_pages * c->page_tokens;
+  t.kv_max = max_keys(c, a);
+  t.page_shift = page_shift(c);
   t.scale_log2e = a->scale * kLog2e;
-  TREVS_HIP(launch_kv8_attention(t, a->dtype, c->d_head, c->page_tokens, reinterpret_cast<hipStream_t>(stream)));
+  t.part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(ws) + L.part);
+  t.part_ml = reinterpret_cast<float2*>(ws);
+  TREVS_HIP(launch_kv8_attention(t, L.plan, a->dtype, c->d_head, reinterpret_cast<hipStream_t>(stream)));
   return TREVS_OK;
 }
 

@@ -1,106 +1,374 @@
 // Attention of query rows over the 8-bit paged cache: one pass over the keys
-// with the running maximum and sum of the softmax.
+// with the running maximum and sum of the softmax, products on the matrix
+// cores with fp32 sums.
 //
-// A wave takes one query row: lanes hold a token each for the logits, then
-// D/64 channels each for the weighted values.
+// The heads of a group share their keys, so a group's rows (t, g), r = t G + g,
+// are one product.  Logits are formed turned, S^T = K Q^T (rows tokens, columns
+// query rows): the lane of a column then holds the weights of its own query
+// row, in the layout in which the second product, O^T = V^T P^T, takes them as
+// its operand, so they never leave its registers.  That needs the k positions
+// of the second product (tokens) to be dealt to the lanes as the first one's
+// output rows are; which token sits in which row of K is free, so the rows are
+// dealt such that a lane holds 16 tokens in a row: 16 bytes of a value
+// channel, which the cache stores token last for this.
+//
+// e4m3 numbers are bf16 numbers, so keys and values enter the products
+// exactly.  bf16 queries do too; the weights are rounded to bf16 (2^-9 of
+// each, random in sign, below the output's own rounding).  fp32 queries and
+// weights are split into three bf16 parts, 24 bits.
 #include "cache.hpp"
 
 namespace trevs {
 namespace {
 
-template <class E, int D, int PAGE>
-__global__ __launch_bounds__(64) void row_kernel(AttnArgs a) {
-  __shared__ float q[D];
-  __shared__ float w[64];
-  const int lane = threadIdx.x;
-  int id = blockIdx.x;
-  const int h = id % a.H_q;
-  id /= a.H_q;
-  const int t = id % a.T_max, b = id / a.T_max;
-  const int rows = a.q_len ? min(max(a.q_len[b], 0), a.T_max) : a.T_max;
-  if (t >= rows) return;
-  const int slot = slot_of(a.slots, b, a.c.n_slots);
-  const int L = slot_len(a.c.len, slot, a.kv_max);
-  const int n = a.causal ? min(L - rows + t + 1, L) : L;
-  const size_t row = (size_t)b * a.T_max + t;
-  for (int c = lane; c < D; c += 64) q[c] = load_scalar(a.q, row * a.q_ld + (size_t)h * D + c, E()) * a.scale_log2e;
-  __syncthreads();
-  float m = -INFINITY, sum = 0.f, acc[D / 64];
-#pragma unroll
-  for (int k = 0; k < D / 64; ++k) acc[k] = 0.f;
-  for (int j0 = 0; j0 < n; j0 += 64) {
-    const int j = j0 + lane;
-    const int page = j < n ? page_at(a.c, slot, j / PAGE) : -1;
-    const size_t block = (size_t)max(page, 0) * a.c.H_kv + h / a.G;
-    float s = -INFINITY;
-    if (page >= 0) {
-      const uint32_t* k = reinterpret_cast<const uint32_t*>(a.c.k + block * (PAGE * D) + (j % PAGE) * D);
-      float x = 0.f, y[4];
-      for (int c = 0; c < D / 4; ++c) {
-        from_e4m3(k[c], y);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x = fmaf(q[4 * c + i], y[i], x);
-      }
-      s = x * a.c.k_scale[block];
-    }
-    const float top = fmaxf(m, wave_max(s));
-    if (top == -INFINITY) continue;
-    const float old = exp2f(m - top), p = exp2f(s - top);
-    m = top;
-    sum = sum * old + wave_sum(p);
-    __syncthreads();
-    w[lane] = page >= 0 ? p * a.c.v_scale[block] : 0.f;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < D / 64; ++k) acc[k] *= old;
-    for (int i = 0; i < min(64, n - j0); ++i) {
-      const int pg = page_at(a.c, slot, (j0 + i) / PAGE);
-      if (pg < 0) continue;
-      const uint8_t* v = a.c.v + ((size_t)pg * a.c.H_kv + h / a.G) * (PAGE * D) + (j0 + i) % PAGE;
-#pragma unroll
-      for (int k = 0; k < D / 64; ++k) {
-        float y[4];
-        from_e4m3(v[(lane + 64 * k) * PAGE], y);
-        acc[k] = fmaf(w[i], y[0], acc[k]);
-      }
-    }
-  }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
-#pragma unroll
-  for (int k = 0; k < D / 64; ++k) {
-    const size_t o = (row * a.H_q + h) * D + lane + 64 * k;
-    if (E::kBytes == 2)
-      reinterpret_cast<__bf16*>(a.out)[o] = (__bf16)(acc[k] * inv);
-    else
-      reinterpret_cast<float*>(a.out)[o] = acc[k] * inv;
-  }
-  if (a.lse && lane == 0)
-    a.lse[((size_t)b * a.H_q + h) * a.T_max + t] = sum > 0.f ? (m + log2f(sum)) * kLn2 : -INFINITY;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+template <class E>
+constexpr int kParts = E::kBytes == 2 ? 1 : 3;
+
+// Eight e4m3 numbers, times a power of two, as bf16.
+__device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-template <class E, int D>
-void by_page(const AttnArgs& a, int page, hipStream_t s) {
-  const dim3 grid((unsigned)((long long)a.B * a.T_max * a.H_q));
-  if (page == 16) hipLaunchKernelGGL((row_kernel<E, D, 16>), grid, dim3(64), 0, s, a);
-  if (page == 32) hipLaunchKernelGGL((row_kernel<E, D, 32>), grid, dim3(64), 0, s, a);
-  if (page == 64) hipLaunchKernelGGL((row_kernel<E, D, 64>), grid, dim3(64), 0, s, a);
+// Eight fp32 values as bf16 parts that sum to them (one part: rounded).
+template <int N>
+__device__ __forceinline__ void split_parts(float (&x)[8], bf16x8 (&out)[N]) {
+#pragma unroll
+  for (int p = 0; p < N; ++p)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      out[p][j] = (__bf16)x[j];
+      x[j] -= (float)out[p][j];
+    }
+}
+
+__device__ __forceinline__ void load_row8(const void* q, size_t i, float (&x)[8], BF16) {
+  const u32x4 w = ldg16(reinterpret_cast<const uint16_t*>(q) + i);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    x[2 * j] = bf16_lo(w[j]);
+    x[2 * j + 1] = bf16_hi(w[j]);
+  }
+}
+__device__ __forceinline__ void load_row8(const void* q, size_t i, float (&x)[8], F32) {
+  const float* f = reinterpret_cast<const float*>(q) + i;
+  const u32x4 a = ldg16(f), b = ldg16(f + 4);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    x[j] = __uint_as_float(a[j]);
+    x[4 + j] = __uint_as_float(b[j]);
+  }
+}
+
+// Bytes [0, n) of a 16-byte vector kept, the others zeroed.
+__device__ __forceinline__ u32x4 keep_bytes(u32x4 v, int n) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int k = n - 4 * w;
+    v[w] = k >= 4 ? v[w] : k <= 0 ? 0u : v[w] & ((1u << (8 * k)) - 1u);
+  }
+  return v;
 }
 
 template <class E>
-void by_head(const AttnArgs& a, int d_head, int page, hipStream_t s) {
-  if (d_head == 64) by_page<E, 64>(a, page, s);
-  if (d_head == 128) by_page<E, 128>(a, page, s);
-  if (d_head == 256) by_page<E, 256>(a, page, s);
+__device__ __forceinline__ void store4(void* out, size_t i, const float (&x)[4], E) {
+  if constexpr (E::kBytes == 2) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    bf16x4 y;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = (__bf16)x[j];
+    *reinterpret_cast<bf16x4*>(reinterpret_cast<uint16_t*>(out) + i) = y;
+  } else {
+    *reinterpret_cast<float4*>(reinterpret_cast<float*>(out) + i) = make_float4(x[0], x[1], x[2], x[3]);
+  }
+}
+
+constexpr int kUnit = 64;    // tokens of one step of a wave
+constexpr int kWaves = 4;
+
+// A workgroup takes 16 NQ rows of one group and one part of its keys; its
+// waves take every kWaves-th unit of 64 tokens.  Nothing is staged: a lane
+// loads its own 16 bytes of key channels and of value tokens.  Bound by the
+// cache's bytes for single tokens.
+template <class E, int D, int NQ>
+__global__ __launch_bounds__(kWaves * 64) void rows_kernel(AttnArgs a) {
+  constexpr int NP = kParts<E>;
+  constexpr int R = 16 * NQ;
+  __shared__ float s_o[R][D + 4];
+  __shared__ float s_m[kWaves][R], s_l[kWaves][R];
+  const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int id = blockIdx.x;
+  const int split = id % a.n_split;
+  id /= a.n_split;
+  const int rt = id % a.row_tiles;
+  id /= a.row_tiles;
+  const int hk = id % a.c.H_kv, b = id / a.c.H_kv;
+  const int rows = a.q_len ? min(max(a.q_len[b], 0), a.T_max) : a.T_max;
+  const int n_rows = rows * a.G, r0 = rt * R;
+  if (r0 >= n_rows) return;
+  const int slot = slot_of(a.slots, b, a.c.n_slots);
+  const int L = slot_len(a.c.len, slot, a.kv_max);
+  // keys of the tile's last row, and of this workgroup
+  const int t_last = min(r0 + R - 1, n_rows - 1) / a.G;
+  const int n_keys = max(a.causal ? min(L - rows + t_last + 1, L) : L, 0);
+  const int units = (n_keys + kUnit - 1) / kUnit, per = (units + a.n_split - 1) / a.n_split;
+  const int u0 = split * per, u1 = min(u0 + per, units);
+
+  int lim[NQ];  // keys that this lane's query row sees
+  bf16x8 q[NQ][D / 32][NP];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const int r = r0 + 16 * i + n16, t = r / a.G, g = r - t * a.G;
+    lim[i] = r < n_rows ? (a.causal ? min(L - rows + t + 1, L) : L) : 0;
+    const size_t at = ((size_t)b * a.T_max + t) * a.q_ld + (size_t)(hk * a.G + g) * D;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      // lane group g4 holds channels 64 (c/2) + 16 g4 + 8 (c%2) .. +7, as the keys' 16-byte loads give them
+      float x[8] = {};
+      if (r < n_rows) load_row8(a.q, at + c / 2 * 64 + 16 * g4 + 8 * (c & 1), x, E());
+      split_parts<NP>(x, q[i][c]);
+    }
+  }
+  int lim_all = lim[0];
+#pragma unroll
+  for (int i = 1; i < NQ; ++i) lim_all = min(lim_all, lim[i]);
+
+  f32x4 o[NQ][D / 16];
+  float m[NQ], l[NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) o[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int shift = a.page_shift, page_mask = (1 << shift) - 1;
+  const size_t page_bytes = (size_t)D << shift;
+  for (int u = u0 + wave; u < u1; u += kWaves) {
+    // this lane's 16 tokens (weights, values) and the token of its key rows: row 4 y + i of tile t
+    // is token 16 y + 4 t + i
+    const int tok = u * kUnit + 16 * g4, ktok = u * kUnit + 16 * (n16 >> 2) + (n16 & 3);
+    const int page_v = tok < n_keys ? page_at(a.c, slot, tok >> shift) : -1;
+    const int page_k = (ktok & ~15) < n_keys ? page_at(a.c, slot, ktok >> shift) : -1;
+    const size_t block_v = (size_t)max(page_v, 0) * a.c.H_kv + hk, block_k = (size_t)max(page_k, 0) * a.c.H_kv + hk;
+    const uint8_t* kp = a.c.k + block_k * page_bytes + (size_t)(ktok & page_mask) * D + 16 * g4;
+    const uint8_t* vp = a.c.v + block_v * page_bytes + ((size_t)n16 << shift) + (tok & page_mask);
+    u32x4 kw[4][D / 64], vw[D / 16];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) kw[t][c] = ldg16(kp + t * 4 * D + c * 64);
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) vw[c] = ldg16(vp + ((size_t)(16 * c) << shift));
+    float ks = a.c.k_scale[block_v], vs = a.c.v_scale[block_v];
+    const bool whole = __all(page_v >= 0 && u * kUnit + kUnit <= lim_all);
+    f32x4 s[NQ][4];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) {
+        const bf16x8 k0 = widen(kw[t][c][0], kw[t][c][1], 1.f), k1 = widen(kw[t][c][2], kw[t][c][3], 1.f);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i)
+#pragma unroll
+          for (int p = NP - 1; p >= 0; --p) {
+            s[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[i][2 * c][p], s[i][t], 0, 0, 0);
+            s[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[i][2 * c + 1][p], s[i][t], 0, 0, 0);
+          }
+      }
+    int n_v = 16;  // tokens of this lane whose values count
+    if (!whole) {
+      n_v = page_v >= 0 ? min(max(L - tok, 0), 16) : 0;
+      if (page_v < 0) ks = vs = 1.f;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) vw[c] = keep_bytes(vw[c], n_v);
+    }
+    bf16x8 pw[NQ][2][NP];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      float x[16], top = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = s[i][e >> 2][e & 3] * (ks * a.scale_log2e);
+      if (!whole) {
+        const int n = page_v >= 0 ? lim[i] - tok : 0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = e < n ? x[e] : -INFINITY;
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, x[e]);
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      top = fmaxf(top, m[i]);
+      const float base = top == -INFINITY ? 0.f : top, old = exp2f(m[i] - base);
+      m[i] = top;
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        x[e] = exp2f(x[e] - base);
+        sum += x[e];
+      }
+      l[i] = l[i] * old + sum;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) o[i][c] *= old;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = x[8 * h + j];
+        split_parts<NP>(y, pw[i][h]);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+      const bf16x8 v0 = widen(vw[c][0], vw[c][1], vs), v1 = widen(vw[c][2], vw[c][3], vs);
+#pragma unroll
+      for (int i = 0; i < NQ; ++i)
+#pragma unroll
+        for (int p = NP - 1; p >= 0; --p) {
+          o[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pw[i][0][p], o[i][c], 0, 0, 0);
+          o[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pw[i][1][p], o[i][c], 0, 0, 0);
+        }
+    }
+  }
+  // the waves' parts, in their order
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    l[i] += __shfl_xor(l[i], 16, 64);
+    l[i] += __shfl_xor(l[i], 32, 64);
+    if (g4 == 0) {
+      s_m[wave][16 * i + n16] = m[i];
+      s_l[wave][16 * i + n16] = l[i];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][16 * i + n16]);
+    const float f = m[i] == -INFINITY ? 0.f : exp2f(m[i] - top);
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) o[i][c] *= f;
+  }
+  for (int w = 0; w < kWaves; ++w) {
+    if (wave == w) {
+#pragma unroll
+      for (int i = 0; i < NQ; ++i)
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+          f32x4* at = reinterpret_cast<f32x4*>(&s_o[16 * i + n16][16 * c + 4 * g4]);
+          *at = w == 0 ? o[i][c] : *at + o[i][c];
+        }
+    }
+    __syncthreads();
+  }
+  for (int e = threadIdx.x; e < R * (D / 4); e += kWaves * 64) {
+    const int r = e / (D / 4), c = e % (D / 4) * 4;
+    if (r0 + r >= n_rows) break;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      if (s_m[w][r] != -INFINITY) sum += s_l[w][r] * exp2f(s_m[w][r] - top);
+    float x[4] = {s_o[r][c], s_o[r][c + 1], s_o[r][c + 2], s_o[r][c + 3]};
+    if (a.n_split > 1) {
+      const size_t part = (((size_t)b * a.c.H_kv + hk) * ((size_t)a.T_max * a.G) + r0 + r) * a.n_split + split;
+      if (top != -INFINITY) *reinterpret_cast<float4*>(a.part + part * D + c) = make_float4(x[0], x[1], x[2], x[3]);
+      if (c == 0) a.part_ml[part] = make_float2(top, sum);
+      continue;
+    }
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] *= inv;
+    const int t = (r0 + r) / a.G, h = hk * a.G + (r0 + r) - t * a.G;
+    store4(a.out, (((size_t)b * a.T_max + t) * a.H_q + h) * D + c, x, E());
+    if (a.lse && c == 0)
+      a.lse[((size_t)b * a.H_q + h) * a.T_max + t] = sum > 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+  }
+}
+
+// The parts of each row's keys joined, in their order.
+template <class E, int D>
+__global__ __launch_bounds__(D / 4) void join_kernel(AttnArgs a) {
+  int id = blockIdx.x;
+  const int r = id % (a.T_max * a.G);
+  id /= a.T_max * a.G;
+  const int hk = id % a.c.H_kv, b = id / a.c.H_kv;
+  const int rows = a.q_len ? min(max(a.q_len[b], 0), a.T_max) : a.T_max;
+  if (r >= rows * a.G) return;
+  const size_t first = (size_t)blockIdx.x * a.n_split;
+  const int c = threadIdx.x * 4;
+  float top = -INFINITY;
+  for (int s = 0; s < a.n_split; ++s) top = fmaxf(top, a.part_ml[first + s].x);
+  float x[4] = {}, sum = 0.f;
+  for (int s = 0; s < a.n_split; ++s) {
+    const float2 ml = a.part_ml[first + s];
+    if (ml.x == -INFINITY) continue;
+    const float f = exp2f(ml.x - top);
+    sum = fmaf(ml.y, f, sum);
+    const float4 y = *reinterpret_cast<const float4*>(a.part + (first + s) * D + c);
+    x[0] = fmaf(y.x, f, x[0]);
+    x[1] = fmaf(y.y, f, x[1]);
+    x[2] = fmaf(y.z, f, x[2]);
+    x[3] = fmaf(y.w, f, x[3]);
+  }
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] *= inv;
+  const int t = r / a.G, h = hk * a.G + r - t * a.G;
+  store4(a.out, (((size_t)b * a.T_max + t) * a.H_q + h) * D + c, x, E());
+  if (a.lse && c == 0)
+    a.lse[((size_t)b * a.H_q + h) * a.T_max + t] = sum > 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+}
+
+template <class E, int D>
+hipError_t launch(AttnArgs a, const AttnPlan& p, hipStream_t s) {
+  a.row_tiles = p.row_tiles;
+  a.n_split = p.n_split;
+  const dim3 grid((unsigned)((long long)a.B * a.c.H_kv * p.row_tiles * p.n_split)), block(kWaves * 64);
+  if constexpr (!(D == 256 && E::kBytes == 4)) {
+    if (p.rows == 32) hipLaunchKernelGGL((rows_kernel<E, D, 2>), grid, block, 0, s, a);
+  }
+  if (p.rows == 16) hipLaunchKernelGGL((rows_kernel<E, D, 1>), grid, block, 0, s, a);
+  if (p.n_split > 1)
+    hipLaunchKernelGGL((join_kernel<E, D>), dim3((unsigned)((long long)a.B * a.c.H_kv * a.T_max * a.G)), dim3(D / 4),
+                       0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_kv8_attention(const AttnArgs& a, int dtype, int d_head, int page, hipStream_t s) {
-  if (dtype == TREVS_BF16)
-    by_head<BF16>(a, d_head, page, s);
-  else
-    by_head<F32>(a, d_head, page, s);
-  return hipGetLastError();
+AttnPlan attn_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtype, int d_head) {
+  AttnPlan p;
+  const long long n_rows = (long long)T_max * G;
+  p.rows = n_rows <= 16 || (d_head == 256 && dtype == TREVS_F32) ? 16 : 32;
+  p.row_tiles = (int)((n_rows + p.rows - 1) / p.rows);
+  const long long wgs = (long long)B * H_kv * p.row_tiles, units = (kv_max + kUnit - 1) / kUnit;
+  p.n_split = (int)std::max(1LL, std::min((2048 + wgs - 1) / wgs, (units + kWaves - 1) / kWaves));
+  return p;
+}
+
+hipError_t launch_kv8_attention(const AttnArgs& a, const AttnPlan& p, int dtype, int d_head, hipStream_t s) {
+  auto by_head = [&](auto e) {
+    using E = decltype(e);
+    if (d_head == 64) return launch<E, 64>(a, p, s);
+    if (d_head == 128) return launch<E, 128>(a, p, s);
+    return launch<E, 256>(a, p, s);
+  };
+  return dtype == TREVS_BF16 ? by_head(BF16()) : by_head(F32());
 }
 
 }  // namespace trevs
