@@ -300,6 +300,222 @@ __global__ __launch_bounds__(kWaves * 64) void rows_kernel(AttnArgs a) {
   }
 }
 
+// ---------------------------------------------------------------- many rows
+// A workgroup takes 128 rows of one group, its waves 32 each, and steps through
+// the keys 64 tokens at a time, staged in LDS as they are stored (8 bits) one
+// step ahead.  Bound by the matrix cores and, next to them, the exponentials.
+constexpr int kTileRows = 128;
+constexpr int kStep = 64;  // tokens
+
+// Weights may pass the running maximum by 2^kSlack before the sums are rescaled
+// to a new one: fp32 sums and bf16 weights do not mind, and rescaling becomes rare.
+constexpr float kSlack = 8.f;
+
+// Permutation of a staged row's 16-byte columns, by the row: eight lanes next
+// to each other read one column of eight rows (of keys: 0-3 and 16-19, as their
+// rows are dealt; of values, whose rows are 64 bytes: 0-7) and must meet 8
+// different ones modulo 128 bytes.
+template <int D>
+__device__ __forceinline__ int key_swizzle(int row) {
+  return D == 64 ? ((row >> 1) & 1) | ((row >> 3) & 2) : (row & 3) | ((row >> 2) & 4);
+}
+__device__ __forceinline__ int value_swizzle(int row) { return (row >> 1) & 3; }
+
+template <int D>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tile_kernel(AttnArgs a) {
+  constexpr int kKeyVecs = kStep * D / 16, kVecs = kKeyVecs / 256;  // 16-byte vectors of a side, and of a thread
+  __shared__ u32x4 s_k[2][kKeyVecs], s_v[2][kKeyVecs];
+  __shared__ float s_ks[2][4], s_vs[2][4];  // scales of each 16 tokens; a negative key scale: absent
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // pairs (b, hk) next to each other: a pair's tiles meet on the XCDs that share its index mod 8;
+  // tiles with the most keys first
+  int id = blockIdx.x;
+  const int pairs = a.B * a.c.H_kv, pair = id % pairs;
+  id /= pairs;
+  const int split = id % a.n_split, rt = a.row_tiles - 1 - id / a.n_split;
+  const int b = pair / a.c.H_kv, hk = pair - b * a.c.H_kv;
+  const int rows = a.q_len ? min(max(a.q_len[b], 0), a.T_max) : a.T_max;
+  const int n_rows = rows * a.G, r0 = rt * kTileRows;
+  if (r0 >= n_rows) return;
+  const int slot = slot_of(a.slots, b, a.c.n_slots);
+  const int L = slot_len(a.c.len, slot, a.kv_max);
+  const int t_last = min(r0 + kTileRows - 1, n_rows - 1) / a.G;
+  const int n_keys = max(a.causal ? min(L - rows + t_last + 1, L) : L, 0);
+  const int steps = (n_keys + kStep - 1) / kStep, per = (steps + a.n_split - 1) / a.n_split;
+  const int u0 = split * per, u1 = min(u0 + per, steps);
+
+  // this lane's query row: half h holds channels 32 (c/2) + 16 h + 8 (c%2) .. +7, as the keys' 16-byte reads give them
+  const int r = r0 + 32 * wave + col, t = r / a.G, g = r - t * a.G;
+  const bool live = r < n_rows;
+  const int lim = live ? (a.causal ? min(L - rows + t + 1, L) : L) : 0;
+  bf16x8 q[D / 16];
+  {
+    const size_t at = ((size_t)b * a.T_max + t) * a.q_ld + (size_t)(hk * a.G + g) * D + 16 * half;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+      q[c] = __builtin_bit_cast(
+          bf16x8, live ? ldg16(reinterpret_cast<const uint16_t*>(a.q) + at + c / 2 * 32 + 8 * (c & 1)) : zero4());
+  }
+  // keys every row of the wave sees
+  const int w_first = r0 + 32 * wave;
+  const int lim_all = w_first + 31 < n_rows ? (a.causal ? min(L - rows + w_first / a.G + 1, L) : L) : 0;
+
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
+  float m = -INFINITY, l = 0.f;
+
+  const int shift = a.page_shift, page_mask = (1 << shift) - 1;
+  const size_t page_bytes = (size_t)D << shift;
+  // Vectors of a step: key vector e holds 16 channels of token e / (D/16), value vector e 16 tokens of
+  // channel e / 4.  In LDS a row's 16-byte columns are permuted by the row so that the lanes of
+  // a read, one row each, meet all banks.
+  u32x4 gk[kVecs], gv[kVecs];
+  float g_ks = -1.f, g_vs = 1.f;
+  auto load = [&](int u) {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int e = tid + 256 * i;
+      const int kt = u * kStep + e / (D / 16), vt = u * kStep + (e & 3) * 16;
+      const int kp = kt < n_keys ? page_at(a.c, slot, kt >> shift) : -1;
+      const int vp = vt < n_keys ? page_at(a.c, slot, vt >> shift) : -1;
+      gk[i] = zero4();
+      gv[i] = zero4();
+      if (kp >= 0)
+        gk[i] = ldg16(a.c.k + ((size_t)kp * a.c.H_kv + hk) * page_bytes + (size_t)(kt & page_mask) * D + e % (D / 16) * 16);
+      if (vp >= 0) {
+        gv[i] = ldg16(a.c.v + ((size_t)vp * a.c.H_kv + hk) * page_bytes + ((size_t)(e >> 2) << shift) + (vt & page_mask));
+        if (vt + 16 > L) gv[i] = keep_bytes(gv[i], L - vt);
+      }
+      if (i == 0 && tid < 4) {  // (e & 3 == tid: the block of these 16 tokens)
+        const size_t block = (size_t)max(vp, 0) * a.c.H_kv + hk;
+        g_ks = vp >= 0 ? a.c.k_scale[block] : -1.f;
+        g_vs = vp >= 0 ? a.c.v_scale[block] : 1.f;
+      }
+    }
+  };
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int e = tid + 256 * i;
+      const int kr = e / (D / 16), kc = e % (D / 16);
+      s_k[buf][kr * (D / 16) + (kc ^ key_swizzle<D>(kr))] = gk[i];
+      const int vr = e >> 2, vc = e & 3;
+      s_v[buf][vr * 4 + (vc ^ value_swizzle(vr))] = gv[i];
+    }
+    if (tid < 4) {
+      s_ks[buf][tid] = g_ks;
+      s_vs[buf][tid] = g_vs;
+    }
+  };
+  if (u0 < u1) {
+    load(u0);
+    store(0);
+  }
+  __syncthreads();
+  for (int u = u0; u < u1; ++u) {
+    const int buf = (u - u0) & 1;
+    if (u + 1 < u1) load(u + 1);
+    f32x16 s[2];
+    float ks[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      ks[y] = s_ks[buf][2 * y + half];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
+      // row 8j + 4h + i of the product is token 16 h + 4 j + i
+      const int kr = 32 * y + 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        const u32x4 w = s_k[buf][kr * (D / 16) + ((2 * c + half) ^ key_swizzle<D>(kr))];
+        s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(w[0], w[1], 1.f), q[2 * c], s[y], 0, 0, 0);
+        s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(w[2], w[3], 1.f), q[2 * c + 1], s[y], 0, 0, 0);
+      }
+    }
+    const bool whole = (u + 1) * kStep <= lim_all && __all(ks[0] >= 0.f && ks[1] >= 0.f);
+    float f[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      f[y] = fabsf(ks[y]) * a.scale_log2e;
+      if (!whole) {
+        const int n = ks[y] >= 0.f ? lim - (u * kStep + 32 * y + 16 * half) : 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[y][i] = i < n ? s[y][i] : -INFINITY;
+      }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      float x = s[y][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) x = fmaxf(x, s[y][i]);
+      top = fmaxf(top, x * f[y]);
+    }
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    if (__any(top > m + kSlack)) {
+      const float now = fmaxf(top, m), old = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
+      m = now;
+      l *= old;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[c][i] *= old;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+    bf16x8 p[4];
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[y][i], f[y], -base));
+        l += x;
+        p[2 * y + (i >> 3)][i & 7] = (__bf16)x;
+      }
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const float vs = s_vs[buf][2 * y + half];
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        const int vr = 32 * c + col;
+        const u32x4 w = s_v[buf][vr * 4 + ((2 * y + half) ^ value_swizzle(vr))];
+        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(w[0], w[1], vs), p[2 * y], o[c], 0, 0, 0);
+        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(w[2], w[3], vs), p[2 * y + 1], o[c], 0, 0, 0);
+      }
+    }
+    if (u + 1 < u1) store(buf ^ 1);
+    __syncthreads();
+  }
+  l += __shfl_xor(l, 32, 64);
+  if (!live) return;
+  if (a.n_split > 1) {
+    const size_t part = ((size_t)pair * ((size_t)a.T_max * a.G) + r) * a.n_split + split;
+    if (half == 0) a.part_ml[part] = make_float2(m, l);
+    if (m == -INFINITY) return;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<float4*>(a.part + part * D + 32 * c + 8 * j + 4 * half) =
+            make_float4(o[c][4 * j], o[c][4 * j + 1], o[c][4 * j + 2], o[c][4 * j + 3]);
+    return;
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const int h = hk * a.G + g;
+  const size_t out = (((size_t)b * a.T_max + t) * a.H_q + h) * D;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float x[4] = {o[c][4 * j] * inv, o[c][4 * j + 1] * inv, o[c][4 * j + 2] * inv, o[c][4 * j + 3] * inv};
+      store4(a.out, out + 32 * c + 8 * j + 4 * half, x, BF16());
+    }
+  if (a.lse && half == 0)
+    a.lse[((size_t)b * a.H_q + h) * a.T_max + t] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+}
+
 // The parts of each row's keys joined, in their order.
 template <class E, int D>
 __global__ __launch_bounds__(D / 4) void join_kernel(AttnArgs a) {
@@ -343,6 +559,9 @@ hipError_t launch(AttnArgs a, const AttnPlan& p, hipStream_t s) {
     if (p.rows == 32) hipLaunchKernelGGL((rows_kernel<E, D, 2>), grid, block, 0, s, a);
   }
   if (p.rows == 16) hipLaunchKernelGGL((rows_kernel<E, D, 1>), grid, block, 0, s, a);
+  if constexpr (E::kBytes == 2) {
+    if (p.rows == kTileRows) hipLaunchKernelGGL((tile_kernel<D>), grid, block, 0, s, a);
+  }
   if (p.n_split > 1)
     hipLaunchKernelGGL((join_kernel<E, D>), dim3((unsigned)((long long)a.B * a.c.H_kv * a.T_max * a.G)), dim3(D / 4),
                        0, s, a);
@@ -354,10 +573,11 @@ hipError_t launch(AttnArgs a, const AttnPlan& p, hipStream_t s) {
 AttnPlan attn_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtype, int d_head) {
   AttnPlan p;
   const long long n_rows = (long long)T_max * G;
-  p.rows = n_rows <= 16 || (d_head == 256 && dtype == TREVS_F32) ? 16 : 32;
+  p.rows = n_rows <= 16 || (d_head == 256 && dtype == TREVS_F32) ? 16 : n_rows <= 32 || dtype == TREVS_F32 ? 32 : kTileRows;
   p.row_tiles = (int)((n_rows + p.rows - 1) / p.rows);
   const long long wgs = (long long)B * H_kv * p.row_tiles, units = (kv_max + kUnit - 1) / kUnit;
-  p.n_split = (int)std::max(1LL, std::min((2048 + wgs - 1) / wgs, (units + kWaves - 1) / kWaves));
+  const long long target = p.rows == kTileRows ? 1024 : 2048;
+  p.n_split = (int)std::max(1LL, std::min((target + wgs - 1) / wgs, (units + kWaves - 1) / kWaves));
   return p;
 }
 

@@ -586,9 +586,14 @@ def _check_list(t, name, device, n=None):
 
 def _call(fn, device, stream, *args):
     """fn(*args, stream) on the tensors' device: with torch's current stream
-    there unless one is given."""
-    with torch.cuda.device(device):
-        st = fn(*args, _stream(stream))
+    there unless one is given (the raw handle: making a Stream object and
+    switching to a device that is current already cost 4 us of a 9 us call)."""
+    if device.index == torch.cuda.current_device():
+        s = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+        st = fn(*args, s)
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, _stream(stream))
     if st:
         raise TrevsError(st, fn.__name__)
 
