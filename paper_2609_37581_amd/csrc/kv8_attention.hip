@@ -368,41 +368,48 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tile_kernel(AttnArgs a)
     for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
   float m = -INFINITY, l = 0.f;
 
-  const int shift = a.page_shift, page_mask = (1 << shift) - 1;
-  const size_t page_bytes = (size_t)D << shift;
   // Vectors of a step: key vector e holds 16 channels of token e / (D/16), value vector e 16 tokens of
-  // channel e / 4.  In LDS a row's 16-byte columns are permuted by the row so that the lanes of
-  // a read, one row each, meet all banks.
+  // channel e / 4.  Their places in a page are the same in every step (64 tokens are whole pages); a
+  // lane looks up the page of its values' 16 tokens a step ahead of the loads, and the key
+  // vectors of a wave lie in one page each, whose number is one of those.  In LDS a row's 16-byte
+  // columns are permuted by the row so that the lanes of a read, one row each, meet all banks.
+  const int shift = a.page_shift, page_mask = (1 << shift) - 1;
+  const size_t page_stride = ((size_t)D << shift) * a.c.H_kv;
+  const uint8_t* k_base = a.c.k + ((size_t)hk * D << shift);
+  const uint8_t* v_base = a.c.v + ((size_t)hk * D << shift) + ((size_t)(tid >> 2) << shift) + ((tid & 3) * 16 & page_mask);
+  const int32_t* table = a.c.table + (size_t)max(slot, 0) * a.c.max_pages;
+  const int last_page = max(n_keys - 1, 0) >> shift;
   u32x4 gk[kVecs], gv[kVecs];
-  float g_ks = -1.f, g_vs = 1.f;
-  auto load = [&](int u) {
+  float g_ks, g_vs;
+  int g_n;  // tokens of this lane's value vectors that count
+  int page = -1;
+  auto look_up = [&](int u) { page = table[min((u * kStep + (tid & 3) * 16) >> shift, last_page)]; };
+  auto load = [&](int u) {  // (after look_up(u))
+    const bool there = page >= 0 && page < a.c.n_pages;
+    const int at = there ? page : 0;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int e = tid + 256 * i;
-      const int kt = u * kStep + e / (D / 16), vt = u * kStep + (e & 3) * 16;
-      const int kp = kt < n_keys ? page_at(a.c, slot, kt >> shift) : -1;
-      const int vp = vt < n_keys ? page_at(a.c, slot, vt >> shift) : -1;
-      gk[i] = zero4();
-      gv[i] = zero4();
-      if (kp >= 0)
-        gk[i] = ldg16(a.c.k + ((size_t)kp * a.c.H_kv + hk) * page_bytes + (size_t)(kt & page_mask) * D + e % (D / 16) * 16);
-      if (vp >= 0) {
-        gv[i] = ldg16(a.c.v + ((size_t)vp * a.c.H_kv + hk) * page_bytes + ((size_t)(e >> 2) << shift) + (vt & page_mask));
-        if (vt + 16 > L) gv[i] = keep_bytes(gv[i], L - vt);
-      }
-      if (i == 0 && tid < 4) {  // (e & 3 == tid: the block of these 16 tokens)
-        const size_t block = (size_t)max(vp, 0) * a.c.H_kv + hk;
-        g_ks = vp >= 0 ? a.c.k_scale[block] : -1.f;
-        g_vs = vp >= 0 ? a.c.v_scale[block] : 1.f;
-      }
+      const int e = tid + 256 * i, first = (64 * wave + 256 * i) / (D / 16);  // tokens of the vector, of the wave's first
+      const int p = __builtin_amdgcn_readlane(at, first >> 4);
+      gk[i] = ldg16(k_base + (size_t)p * page_stride + ((e / (D / 16)) & page_mask) * D + e % (D / 16) * 16);
     }
+    const uint8_t* v = v_base + (size_t)at * page_stride;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) gv[i] = ldg16(v + ((size_t)(64 * i) << shift));
+    const size_t block = (size_t)at * a.c.H_kv + hk;
+    g_ks = a.c.k_scale[block];
+    g_vs = a.c.v_scale[block];
+    g_n = there ? L - (u * kStep + (tid & 3) * 16) : 0;
+    if (!there) g_ks = -1.f, g_vs = 1.f;
   };
   auto store = [&](int buf) {
+    const bool mask = __any(g_n < 16);
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
       const int e = tid + 256 * i;
       const int kr = e / (D / 16), kc = e % (D / 16);
       s_k[buf][kr * (D / 16) + (kc ^ key_swizzle<D>(kr))] = gk[i];
+      if (mask) gv[i] = keep_bytes(gv[i], g_n);
       const int vr = e >> 2, vc = e & 3;
       s_v[buf][vr * 4 + (vc ^ value_swizzle(vr))] = gv[i];
     }
@@ -412,13 +419,18 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tile_kernel(AttnArgs a)
     }
   };
   if (u0 < u1) {
+    look_up(u0);
     load(u0);
+    look_up(u0 + 1);
     store(0);
   }
+  wait_vmem<0>();  // (the queries too: the loop then waits for its own loads only)
   __syncthreads();
   for (int u = u0; u < u1; ++u) {
     const int buf = (u - u0) & 1;
-    if (u + 1 < u1) load(u + 1);
+    // (past the last step: its own pages again, not used)
+    load(u + 1);
+    look_up(u + 2);
     f32x16 s[2];
     float ks[2];
 #pragma unroll
@@ -485,7 +497,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tile_kernel(AttnArgs a)
         o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(w[2], w[3], vs), p[2 * y + 1], o[c], 0, 0, 0);
       }
     }
-    if (u + 1 < u1) store(buf ^ 1);
+    store(buf ^ 1);
     __syncthreads();
   }
   l += __shfl_xor(l, 32, 64);
