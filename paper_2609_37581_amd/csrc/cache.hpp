@@ -154,14 +154,15 @@ struct AttnArgs {
   float* lse;
   int B, T_max, H_q, G, causal, kv_max, page_shift;
   float scale_log2e;
-  int row_tiles, n_split;
-  float* part;              // n_split > 1: [B,H_kv,T_max*G,n_split,D] sums not yet divided
-  float2* part_ml;          // and [B,H_kv,T_max*G,n_split] (maximum, sum), base 2
+  int row_tiles;
+  float* part;              // cut calls (else null): [2 pieces,rows,D] sums of a workgroup's pieces
+  float2* part_ml;          // [2 pieces,rows] their (maximum, sum), base 2
 };
 // Launch shape of one problem size.
 struct AttnPlan {
-  int rows;                 // query rows of a workgroup
-  int row_tiles, n_split;
+  int rows;                 // query rows of a tile
+  int row_tiles;
+  int pieces;               // workgroups that the steps of all tiles are cut for, 0: a tile to a workgroup
 };
 AttnPlan attn_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtype, int d_head);
 hipError_t launch_kv8_attention(const AttnArgs& a, const AttnPlan& p, int dtype, int d_head, hipStream_t s);

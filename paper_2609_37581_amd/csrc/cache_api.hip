@@ -193,7 +193,7 @@ int max_keys(const trevs_kv8_cache* c, const trevs_kv8_attention_args* a) {
   return a->kv_max ? a->kv_max : c->max_pages * c->page_tokens;
 }
 
-// Parts of split rows: (maximum, sum) pairs, then the sums of values.
+// Sums of cut tiles: (maximum, sum) pairs, then the sums of values.
 struct AttnLayout {
   AttnPlan plan;
   size_t part, total;
@@ -201,7 +201,7 @@ struct AttnLayout {
 AttnLayout attention_layout(const trevs_kv8_cache* c, const trevs_kv8_attention_args* a) {
   AttnLayout L;
   L.plan = attn_plan(a->B, a->T_max, c->H_kv, a->H_q / c->H_kv, max_keys(c, a), a->dtype, c->d_head);
-  const size_t parts = L.plan.n_split > 1 ? (size_t)a->B * a->T_max * a->H_q * L.plan.n_split : 0;
+  const size_t parts = (size_t)2 * L.plan.pieces * L.plan.rows;
   L.part = align_up(parts * sizeof(float2));
   L.total = std::max(L.part + align_up(parts * c->d_head * sizeof(float)), kWsAlign);
   return L;

@@ -89,37 +89,179 @@ __device__ __forceinline__ void store4(void* out, size_t i, const float (&x)[4],
   }
 }
 
-constexpr int kUnit = 64;    // tokens of one step of a wave
+// Weights may pass the running maximum by 2^kSlack before the sums are rescaled
+// to a new one: fp32 sums and bf16 weights do not mind, and rescaling becomes rare.
+constexpr float kSlack = 8.f;
+
+constexpr int kStep = 64;  // tokens of a step
+
+// A tile is R query rows (t, g) of one group; its steps are the 64-token blocks
+// that its last row sees.  Calls of few tiles, or of uneven ones, cut the
+// steps of all of them, one after the other (sequences, row tiles, groups),
+// into gridDim.x equal pieces, a workgroup to a piece: a piece that covers a
+// tile finishes it, the others leave their sums to join_kernel.
+struct Tile {
+  int b, hk, rt;
+};
+struct Sequence {
+  int rows, slot, L;  // query rows, slot, tokens
+};
+__device__ __forceinline__ Sequence sequence(const AttnArgs& a, int b) {
+  Sequence s;
+  s.rows = a.q_len ? min(max(a.q_len[b], 0), a.T_max) : a.T_max;
+  s.slot = slot_of(a.slots, b, a.c.n_slots);
+  s.L = slot_len(a.c.len, s.slot, a.kv_max);
+  return s;
+}
+// Keys that the last row of a tile sees (0 for a tile without rows).
+template <int R>
+__device__ __forceinline__ int tile_keys(const AttnArgs& a, const Sequence& s, int rt) {
+  const int n_rows = s.rows * a.G, r0 = rt * R;
+  if (r0 >= n_rows) return 0;
+  const int t_last = min(r0 + R - 1, n_rows - 1) / a.G;
+  return max(a.causal ? min(s.L - s.rows + t_last + 1, s.L) : s.L, 0);
+}
+__device__ __forceinline__ int steps_of(int keys) { return (keys + kStep - 1) / kStep; }
+
+// The steps of all sequences in one row, held by a wave: lane i of `ends` the
+// end of sequence i's among the first 64 sequences (the rest is recomputed:
+// its loads hit the cache).  The host sees to it that the sum fits 31 bits.
+template <int R>
+struct Schedule {
+  int ends, total;
+  static __device__ __forceinline__ int scan(const AttnArgs& a, int b0) {
+    const int lane = threadIdx.x & 63, b = b0 + lane;
+    int n = 0;
+    if (b < a.B) {
+      const Sequence s = sequence(a, b);
+      for (int rt = 0; rt * R < s.rows * a.G; ++rt) n += steps_of(tile_keys<R>(a, s, rt));
+    }
+    return wave_incl_scan(n * a.c.H_kv, lane);
+  }
+  __device__ __forceinline__ void init(const AttnArgs& a) {
+    ends = scan(a, 0);
+    total = __builtin_amdgcn_readlane(ends, 63);
+    for (int b0 = 64; b0 < a.B; b0 += 64) total += __builtin_amdgcn_readlane(scan(a, b0), 63);
+  }
+  // The first step of workgroup w of n.
+  __device__ __forceinline__ int start(int w, int n) const { return (int)((long long)w * total / n); }
+  // The workgroup that holds a step.
+  __device__ __forceinline__ int owner(int step, int n) const {
+    int w = (int)((long long)step * n / total);
+    while (start(w + 1, n) <= step) ++w;
+    return w;
+  }
+  // Where sequence b's steps begin.
+  __device__ __forceinline__ int begin(const AttnArgs& a, int b) const {
+    if (b == 0) return 0;
+    int before = 0, e = ends;
+    for (int b0 = 0;; b0 += 64) {
+      if (b0) e = scan(a, b0);
+      if (b <= b0 + 64) return before + __builtin_amdgcn_readlane(e, b - 1 - b0);
+      before += __builtin_amdgcn_readlane(e, 63);
+    }
+  }
+  // The tile that holds a step, and the tile's first step.
+  __device__ __forceinline__ Tile find(const AttnArgs& a, int step, int& first) const {
+    int before = 0, e = ends, b0 = 0;
+    while (before + __builtin_amdgcn_readlane(e, 63) <= step) {
+      before += __builtin_amdgcn_readlane(e, 63);
+      b0 += 64;
+      e = scan(a, b0);
+    }
+    const int i = __builtin_ctzll(__ballot(before + e > step));
+    Tile t;
+    t.b = b0 + i;
+    first = before + (i ? __builtin_amdgcn_readlane(e, i - 1) : 0);
+    const Sequence s = sequence(a, t.b);
+    for (t.rt = 0;; ++t.rt) {
+      const int n = steps_of(tile_keys<R>(a, s, t.rt));
+      if (step < first + n * a.c.H_kv) {
+        t.hk = (step - first) / n;
+        first += t.hk * n;
+        return t;
+      }
+      first += n * a.c.H_kv;
+    }
+  }
+};
+
+// A workgroup's way through its work: in a cut call the pieces of tiles that its steps cover, else one tile.
+struct Piece {
+  Tile t;
+  int u0, u1;   // steps of the tile
+  int part;     // -1: the whole tile; else where its sums go
+};
+template <int R>
+struct Walk {
+  Schedule<R> s;
+  int at, end;
+  __device__ __forceinline__ explicit Walk(const AttnArgs& a) : at(0), end(1) {
+    if (!a.part) return;
+    s.init(a);
+    at = s.start(blockIdx.x, gridDim.x);
+    end = s.start(blockIdx.x + 1, gridDim.x);
+  }
+  __device__ __forceinline__ bool next(const AttnArgs& a, Piece& p) {
+    if (at >= end) return false;
+    p.part = -1;
+    if (!a.part) {
+      // not cut: groups (b, hk) next to each other, so that a group's tiles meet on the XCDs that share
+      // its index modulo 8; the tiles with the most keys first
+      const int groups = a.B * a.c.H_kv, group = blockIdx.x % groups;
+      p.t.rt = a.row_tiles - 1 - blockIdx.x / groups;
+      p.t.b = group / a.c.H_kv;
+      p.t.hk = group - p.t.b * a.c.H_kv;
+      p.u0 = 0;
+      p.u1 = steps_of(tile_keys<R>(a, sequence(a, p.t.b), p.t.rt));
+      at = end;
+      return true;
+    }
+    int first;
+    p.t = s.find(a, at, first);
+    const int n = steps_of(tile_keys<R>(a, sequence(a, p.t.b), p.t.rt));
+    p.u0 = at - first;
+    p.u1 = min(n, end - first);
+    // a piece that begins its tile is the workgroup's last, one that does not its first
+    if (p.u0 != 0 || p.u1 != n) p.part = 2 * blockIdx.x + (p.u0 == 0);
+    at = first + p.u1;
+    return true;
+  }
+};
+
+__device__ __forceinline__ size_t out_row(const AttnArgs& a, const Tile& t, int r) {
+  const int q = r / a.G, h = t.hk * a.G + r - q * a.G;
+  return ((size_t)t.b * a.T_max + q) * a.H_q + h;
+}
+__device__ __forceinline__ void store_lse(const AttnArgs& a, const Tile& t, int r, float m, float l) {
+  const int q = r / a.G, h = t.hk * a.G + r - q * a.G;
+  a.lse[((size_t)t.b * a.H_q + h) * a.T_max + q] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+}
+
 constexpr int kWaves = 4;
 
-// A workgroup takes 16 NQ rows of one group and one part of its keys; its
-// waves take every kWaves-th unit of 64 tokens.  Nothing is staged: a lane
-// loads its own 16 bytes of key channels and of value tokens.  Bound by the
-// cache's bytes for single tokens.
+// A workgroup takes 16 NQ rows of one group; its waves take every kWaves-th
+// step.  Nothing is staged: a lane loads its own 16 bytes of key channels and
+// of value tokens.  Bound by the cache's bytes for single tokens.
 template <class E, int D, int NQ>
-__global__ __launch_bounds__(kWaves * 64) void rows_kernel(AttnArgs a) {
+struct RowsShared {
+  float o[16 * NQ][D + 4];
+  float m[kWaves][16 * NQ], l[kWaves][16 * NQ];
+};
+
+template <class E, int D, int NQ>
+__device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, RowsShared<E, D, NQ>& sh) {
   constexpr int NP = kParts<E>;
   constexpr int R = 16 * NQ;
-  __shared__ float s_o[R][D + 4];
-  __shared__ float s_m[kWaves][R], s_l[kWaves][R];
+  auto& s_o = sh.o;
+  auto& s_m = sh.m;
+  auto& s_l = sh.l;
   const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int id = blockIdx.x;
-  const int split = id % a.n_split;
-  id /= a.n_split;
-  const int rt = id % a.row_tiles;
-  id /= a.row_tiles;
-  const int hk = id % a.c.H_kv, b = id / a.c.H_kv;
-  const int rows = a.q_len ? min(max(a.q_len[b], 0), a.T_max) : a.T_max;
-  const int n_rows = rows * a.G, r0 = rt * R;
-  if (r0 >= n_rows) return;
-  const int slot = slot_of(a.slots, b, a.c.n_slots);
-  const int L = slot_len(a.c.len, slot, a.kv_max);
-  // keys of the tile's last row, and of this workgroup
-  const int t_last = min(r0 + R - 1, n_rows - 1) / a.G;
-  const int n_keys = max(a.causal ? min(L - rows + t_last + 1, L) : L, 0);
-  const int units = (n_keys + kUnit - 1) / kUnit, per = (units + a.n_split - 1) / a.n_split;
-  const int u0 = split * per, u1 = min(u0 + per, units);
+  const int b = pc.t.b, hk = pc.t.hk, r0 = pc.t.rt * R, u0 = pc.u0, u1 = pc.u1;
+  const Sequence seq = sequence(a, b);
+  const int rows = seq.rows, slot = seq.slot, L = seq.L, n_rows = rows * a.G;
+  const int n_keys = tile_keys<R>(a, seq, pc.t.rt);
 
   int lim[NQ];  // keys that this lane's query row sees
   bf16x8 q[NQ][D / 32][NP];
@@ -150,17 +292,24 @@ __global__ __launch_bounds__(kWaves * 64) void rows_kernel(AttnArgs a) {
     for (int c = 0; c < D / 16; ++c) o[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
+  // A lane looks up the page of its 16 tokens (weights, values) a unit ahead; its key rows, of tile t
+  // row 4 y + i = token 16 y + 4 t + i, lie in the page of lane group y.  Their places in a page are the
+  // same in every unit (64 tokens are whole pages).
   const int shift = a.page_shift, page_mask = (1 << shift) - 1;
-  const size_t page_bytes = (size_t)D << shift;
+  const size_t page_stride = ((size_t)D << shift) * a.c.H_kv;
+  const int key_row = (16 * (n16 >> 2) & page_mask) + (n16 & 3);
+  const uint8_t* k_base = a.c.k + ((size_t)hk * D << shift) + key_row * D + 16 * g4;
+  const uint8_t* v_base = a.c.v + ((size_t)hk * D << shift) + ((size_t)n16 << shift) + (16 * g4 & page_mask);
+  const int32_t* table = a.c.table + (size_t)max(slot, 0) * a.c.max_pages;
+  const int last_page = max(n_keys - 1, 0) >> shift;
+  auto look_up = [&](int u) { return table[min((u * kStep + 16 * g4) >> shift, last_page)]; };
+  int next = u0 + wave < u1 ? look_up(u0 + wave) : -1;
   for (int u = u0 + wave; u < u1; u += kWaves) {
-    // this lane's 16 tokens (weights, values) and the token of its key rows: row 4 y + i of tile t
-    // is token 16 y + 4 t + i
-    const int tok = u * kUnit + 16 * g4, ktok = u * kUnit + 16 * (n16 >> 2) + (n16 & 3);
-    const int page_v = tok < n_keys ? page_at(a.c, slot, tok >> shift) : -1;
-    const int page_k = (ktok & ~15) < n_keys ? page_at(a.c, slot, ktok >> shift) : -1;
-    const size_t block_v = (size_t)max(page_v, 0) * a.c.H_kv + hk, block_k = (size_t)max(page_k, 0) * a.c.H_kv + hk;
-    const uint8_t* kp = a.c.k + block_k * page_bytes + (size_t)(ktok & page_mask) * D + 16 * g4;
-    const uint8_t* vp = a.c.v + block_v * page_bytes + ((size_t)n16 << shift) + (tok & page_mask);
+    const int tok = u * kStep + 16 * g4;
+    const bool there = next >= 0 && next < a.c.n_pages && tok < n_keys;
+    const int page = there ? next : 0;
+    const uint8_t* kp = k_base + (size_t)__shfl(page, 16 * (n16 >> 2), 64) * page_stride;
+    const uint8_t* vp = v_base + (size_t)page * page_stride;
     u32x4 kw[4][D / 64], vw[D / 16];
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -168,8 +317,10 @@ __global__ __launch_bounds__(kWaves * 64) void rows_kernel(AttnArgs a) {
       for (int c = 0; c < D / 64; ++c) kw[t][c] = ldg16(kp + t * 4 * D + c * 64);
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) vw[c] = ldg16(vp + ((size_t)(16 * c) << shift));
-    float ks = a.c.k_scale[block_v], vs = a.c.v_scale[block_v];
-    const bool whole = __all(page_v >= 0 && u * kUnit + kUnit <= lim_all);
+    const size_t block = (size_t)page * a.c.H_kv + hk;
+    float ks = a.c.k_scale[block], vs = a.c.v_scale[block];
+    next = look_up(u + kWaves);
+    const bool whole = __all(there && u * kStep + kStep <= lim_all);
     f32x4 s[NQ][4];
 #pragma unroll
     for (int i = 0; i < NQ; ++i)
@@ -188,10 +339,10 @@ __global__ __launch_bounds__(kWaves * 64) void rows_kernel(AttnArgs a) {
             s[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[i][2 * c + 1][p], s[i][t], 0, 0, 0);
           }
       }
-    int n_v = 16;  // tokens of this lane whose values count
     if (!whole) {
-      n_v = page_v >= 0 ? min(max(L - tok, 0), 16) : 0;
-      if (page_v < 0) ks = vs = 1.f;
+      const int n_v =  // tokens of this lane whose values count
+           there ? min(max(L - tok, 0), 16) : 0;
+      if (!there) ks = vs = 1.f;
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) vw[c] = keep_bytes(vw[c], n_v);
     }
@@ -202,7 +353,7 @@ __global__ __launch_bounds__(kWaves * 64) void rows_kernel(AttnArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) x[e] = s[i][e >> 2][e & 3] * (ks * a.scale_log2e);
       if (!whole) {
-        const int n = page_v >= 0 ? lim[i] - tok : 0;
+        const int n = there ? lim[i] - tok : 0;
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[e] = e < n ? x[e] : -INFINITY;
       }
@@ -210,18 +361,19 @@ __global__ __launch_bounds__(kWaves * 64) void rows_kernel(AttnArgs a) {
       for (int e = 0; e < 16; ++e) top = fmaxf(top, x[e]);
       top = fmaxf(top, __shfl_xor(top, 16, 64));
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      top = fmaxf(top, m[i]);
-      const float base = top == -INFINITY ? 0.f : top, old = exp2f(m[i] - base);
-      m[i] = top;
-      float sum = 0.f;
+      if (__any(top > m[i] + kSlack)) {
+        const float now = fmaxf(top, m[i]), old = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - now);
+        m[i] = now;
+        l[i] *= old;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) o[i][c] *= old;
+      }
+      const float base = m[i] == -INFINITY ? 0.f : m[i];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        x[e] = exp2f(x[e] - base);
-        sum += x[e];
+        x[e] = __builtin_amdgcn_exp2f(x[e] - base);
+        l[i] += x[e];
       }
-      l[i] = l[i] * old + sum;
-#pragma unroll
-      for (int c = 0; c < D / 16; ++c) o[i][c] *= old;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float y[8];
@@ -284,19 +436,28 @@ __global__ __launch_bounds__(kWaves * 64) void rows_kernel(AttnArgs a) {
     for (int w = 0; w < kWaves; ++w)
       if (s_m[w][r] != -INFINITY) sum += s_l[w][r] * exp2f(s_m[w][r] - top);
     float x[4] = {s_o[r][c], s_o[r][c + 1], s_o[r][c + 2], s_o[r][c + 3]};
-    if (a.n_split > 1) {
-      const size_t part = (((size_t)b * a.c.H_kv + hk) * ((size_t)a.T_max * a.G) + r0 + r) * a.n_split + split;
-      if (top != -INFINITY) *reinterpret_cast<float4*>(a.part + part * D + c) = make_float4(x[0], x[1], x[2], x[3]);
+    if (pc.part >= 0) {
+      const size_t part = (size_t)pc.part * R + r;
+      *reinterpret_cast<float4*>(a.part + part * D + c) = make_float4(x[0], x[1], x[2], x[3]);
       if (c == 0) a.part_ml[part] = make_float2(top, sum);
       continue;
     }
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] *= inv;
-    const int t = (r0 + r) / a.G, h = hk * a.G + (r0 + r) - t * a.G;
-    store4(a.out, (((size_t)b * a.T_max + t) * a.H_q + h) * D + c, x, E());
-    if (a.lse && c == 0)
-      a.lse[((size_t)b * a.H_q + h) * a.T_max + t] = sum > 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+    store4(a.out, out_row(a, pc.t, r0 + r) * D + c, x, E());
+    if (a.lse && c == 0) store_lse(a, pc.t, r0 + r, top, sum);
+  }
+}
+
+template <class E, int D, int NQ>
+__global__ __launch_bounds__(kWaves * 64, NQ == 1 && D <= 128 && E::kBytes == 2 ? 3 : 1) void rows_kernel(AttnArgs a) {
+  __shared__ RowsShared<E, D, NQ> sh;
+  Walk<16 * NQ> walk(a);
+  Piece p;
+  while (walk.next(a, p)) {
+    rows_piece<E, D, NQ>(a, p, sh);
+    __syncthreads();  // the sums in LDS are read before the next piece's are written
   }
 }
 
@@ -305,11 +466,6 @@ __global__ __launch_bounds__(kWaves * 64) void rows_kernel(AttnArgs a) {
 // the keys 64 tokens at a time, staged in LDS as they are stored (8 bits) one
 // step ahead.  Bound by the matrix cores and, next to them, the exponentials.
 constexpr int kTileRows = 128;
-constexpr int kStep = 64;  // tokens
-
-// Weights may pass the running maximum by 2^kSlack before the sums are rescaled
-// to a new one: fp32 sums and bf16 weights do not mind, and rescaling becomes rare.
-constexpr float kSlack = 8.f;
 
 // Permutation of a staged row's 16-byte columns, by the row: eight lanes next
 // to each other read one column of eight rows (of keys: 0-3 and 16-19, as their
@@ -322,28 +478,25 @@ __device__ __forceinline__ int key_swizzle(int row) {
 __device__ __forceinline__ int value_swizzle(int row) { return (row >> 1) & 3; }
 
 template <int D>
-__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tile_kernel(AttnArgs a) {
-  constexpr int kKeyVecs = kStep * D / 16, kVecs = kKeyVecs / 256;  // 16-byte vectors of a side, and of a thread
-  __shared__ u32x4 s_k[2][kKeyVecs], s_v[2][kKeyVecs];
-  __shared__ float s_ks[2][4], s_vs[2][4];  // scales of each 16 tokens; a negative key scale: absent
+struct TileShared {
+  static constexpr int kKeyVecs = kStep * D / 16;  // 16-byte vectors of a side
+  u32x4 k[2][kKeyVecs], v[2][kKeyVecs];
+  float ks[2][4], vs[2][4];  // scales of each 16 tokens; a negative key scale: absent
+};
+
+template <int D>
+__device__ __forceinline__ void tile_piece(const AttnArgs& a, const Piece& pc, TileShared<D>& sh) {
+  constexpr int kVecs = TileShared<D>::kKeyVecs / 256;  // of a thread
+  auto& s_k = sh.k;
+  auto& s_v = sh.v;
+  auto& s_ks = sh.ks;
+  auto& s_vs = sh.vs;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // pairs (b, hk) next to each other: a pair's tiles meet on the XCDs that share its index mod 8;
-  // tiles with the most keys first
-  int id = blockIdx.x;
-  const int pairs = a.B * a.c.H_kv, pair = id % pairs;
-  id /= pairs;
-  const int split = id % a.n_split, rt = a.row_tiles - 1 - id / a.n_split;
-  const int b = pair / a.c.H_kv, hk = pair - b * a.c.H_kv;
-  const int rows = a.q_len ? min(max(a.q_len[b], 0), a.T_max) : a.T_max;
-  const int n_rows = rows * a.G, r0 = rt * kTileRows;
-  if (r0 >= n_rows) return;
-  const int slot = slot_of(a.slots, b, a.c.n_slots);
-  const int L = slot_len(a.c.len, slot, a.kv_max);
-  const int t_last = min(r0 + kTileRows - 1, n_rows - 1) / a.G;
-  const int n_keys = max(a.causal ? min(L - rows + t_last + 1, L) : L, 0);
-  const int steps = (n_keys + kStep - 1) / kStep, per = (steps + a.n_split - 1) / a.n_split;
-  const int u0 = split * per, u1 = min(u0 + per, steps);
+  const int b = pc.t.b, hk = pc.t.hk, r0 = pc.t.rt * kTileRows, u0 = pc.u0, u1 = pc.u1;
+  const Sequence seq = sequence(a, b);
+  const int rows = seq.rows, slot = seq.slot, L = seq.L, n_rows = rows * a.G;
+  const int n_keys = tile_keys<kTileRows>(a, seq, pc.t.rt);
 
   // this lane's query row: half h holds channels 32 (c/2) + 16 h + 8 (c%2) .. +7, as the keys' 16-byte reads give them
   const int r = r0 + 32 * wave + col, t = r / a.G, g = r - t * a.G;
@@ -502,10 +655,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tile_kernel(AttnArgs a)
   }
   l += __shfl_xor(l, 32, 64);
   if (!live) return;
-  if (a.n_split > 1) {
-    const size_t part = ((size_t)pair * ((size_t)a.T_max * a.G) + r) * a.n_split + split;
+  if (pc.part >= 0) {
+    const size_t part = (size_t)pc.part * kTileRows + 32 * wave + col;
     if (half == 0) a.part_ml[part] = make_float2(m, l);
-    if (m == -INFINITY) return;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
@@ -515,8 +667,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tile_kernel(AttnArgs a)
     return;
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
-  const int h = hk * a.G + g;
-  const size_t out = (((size_t)b * a.T_max + t) * a.H_q + h) * D;
+  const size_t out = out_row(a, pc.t, r) * D;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c)
 #pragma unroll
@@ -524,59 +675,84 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tile_kernel(AttnArgs a)
       const float x[4] = {o[c][4 * j] * inv, o[c][4 * j + 1] * inv, o[c][4 * j + 2] * inv, o[c][4 * j + 3] * inv};
       store4(a.out, out + 32 * c + 8 * j + 4 * half, x, BF16());
     }
-  if (a.lse && half == 0)
-    a.lse[((size_t)b * a.H_q + h) * a.T_max + t] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+  if (a.lse && half == 0) store_lse(a, pc.t, r, m, l);
 }
 
-// The parts of each row's keys joined, in their order.
-template <class E, int D>
-__global__ __launch_bounds__(D / 4) void join_kernel(AttnArgs a) {
+template <int D>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tile_kernel(AttnArgs a) {
+  __shared__ TileShared<D> sh;
+  Walk<kTileRows> walk(a);
+  Piece p;
+  while (walk.next(a, p)) tile_piece<D>(a, p, sh);  // (a piece ends with its last reads of LDS behind a barrier)
+}
+
+// The sums of the pieces of each cut tile joined, in the order of its steps; zeros for rows that see no key.
+constexpr int kJoinThreads = 256;
+template <class E, int D, int R>
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(AttnArgs a, int n_pieces) {
+  constexpr int kRows = kJoinThreads / (D / 4);  // rows of a workgroup, all of one tile
+  Tile t;
   int id = blockIdx.x;
-  const int r = id % (a.T_max * a.G);
-  id /= a.T_max * a.G;
-  const int hk = id % a.c.H_kv, b = id / a.c.H_kv;
-  const int rows = a.q_len ? min(max(a.q_len[b], 0), a.T_max) : a.T_max;
-  if (r >= rows * a.G) return;
-  const size_t first = (size_t)blockIdx.x * a.n_split;
-  const int c = threadIdx.x * 4;
-  float top = -INFINITY;
-  for (int s = 0; s < a.n_split; ++s) top = fmaxf(top, a.part_ml[first + s].x);
-  float x[4] = {}, sum = 0.f;
-  for (int s = 0; s < a.n_split; ++s) {
-    const float2 ml = a.part_ml[first + s];
-    if (ml.x == -INFINITY) continue;
-    const float f = exp2f(ml.x - top);
-    sum = fmaf(ml.y, f, sum);
-    const float4 y = *reinterpret_cast<const float4*>(a.part + (first + s) * D + c);
-    x[0] = fmaf(y.x, f, x[0]);
-    x[1] = fmaf(y.y, f, x[1]);
-    x[2] = fmaf(y.z, f, x[2]);
-    x[3] = fmaf(y.w, f, x[3]);
+  const int sub = id % (R / kRows);
+  id /= R / kRows;
+  t.rt = id % a.row_tiles;
+  id /= a.row_tiles;
+  t.b = id / a.c.H_kv;
+  t.hk = id - t.b * a.c.H_kv;
+  const Sequence seq = sequence(a, t.b);
+  const int row = sub * kRows + threadIdx.x / (D / 4), r = t.rt * R + row, c = threadIdx.x % (D / 4) * 4;
+  if (t.rt * R + sub * kRows >= seq.rows * a.G) return;
+  const int n = steps_of(tile_keys<R>(a, seq, t.rt));
+  float x[4] = {}, m = -INFINITY, l = 0.f;
+  if (n > 0) {
+    Schedule<R> s;
+    s.init(a);
+    int first = s.begin(a, t.b);
+    for (int rt = 0; rt < t.rt; ++rt) first += steps_of(tile_keys<R>(a, seq, rt)) * a.c.H_kv;
+    first += t.hk * n;
+    const int w0 = s.owner(first, n_pieces), w1 = s.owner(first + n - 1, n_pieces);
+    if (w0 == w1 || r >= seq.rows * a.G) return;  // (one piece has finished it)
+    // the first piece begins the tile, the others do not
+    auto at = [&](int w) { return (size_t)(2 * w + (w == w0)) * R + row; };
+    for (int w = w0; w <= w1; ++w) m = fmaxf(m, a.part_ml[at(w)].x);
+    for (int w = w0; w <= w1; ++w) {
+      const float2 ml = a.part_ml[at(w)];
+      const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+      l = fmaf(ml.y, f, l);
+      const float4 y = *reinterpret_cast<const float4*>(a.part + at(w) * D + c);
+      x[0] = fmaf(y.x, f, x[0]);
+      x[1] = fmaf(y.y, f, x[1]);
+      x[2] = fmaf(y.z, f, x[2]);
+      x[3] = fmaf(y.w, f, x[3]);
+    }
   }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  if (r >= seq.rows * a.G) return;
+  const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) x[j] *= inv;
-  const int t = r / a.G, h = hk * a.G + r - t * a.G;
-  store4(a.out, (((size_t)b * a.T_max + t) * a.H_q + h) * D + c, x, E());
-  if (a.lse && c == 0)
-    a.lse[((size_t)b * a.H_q + h) * a.T_max + t] = sum > 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+  store4(a.out, out_row(a, t, r) * D + c, x, E());
+  if (a.lse && c == 0) store_lse(a, t, r, m, l);
 }
 
 template <class E, int D>
 hipError_t launch(AttnArgs a, const AttnPlan& p, hipStream_t s) {
   a.row_tiles = p.row_tiles;
-  a.n_split = p.n_split;
-  const dim3 grid((unsigned)((long long)a.B * a.c.H_kv * p.row_tiles * p.n_split)), block(kWaves * 64);
+  if (p.pieces == 0) a.part = nullptr;
+  const long long tiles = (long long)a.B * a.c.H_kv * p.row_tiles;
+  auto go = [&](auto kernel, auto join) {
+    constexpr int kRows = kJoinThreads / (D / 4);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.pieces ? p.pieces : tiles)), dim3(256), 0, s, a);
+    if (p.pieces)
+      hipLaunchKernelGGL(join, dim3((unsigned)(tiles * (p.rows / kRows))), dim3(kJoinThreads), 0, s, a, p.pieces);
+  };
+  static_assert(kWaves * 64 == 256, "one block size");
+  if (p.rows == 16) go(rows_kernel<E, D, 1>, join_kernel<E, D, 16>);
   if constexpr (!(D == 256 && E::kBytes == 4)) {
-    if (p.rows == 32) hipLaunchKernelGGL((rows_kernel<E, D, 2>), grid, block, 0, s, a);
+    if (p.rows == 32) go(rows_kernel<E, D, 2>, join_kernel<E, D, 32>);
   }
-  if (p.rows == 16) hipLaunchKernelGGL((rows_kernel<E, D, 1>), grid, block, 0, s, a);
   if constexpr (E::kBytes == 2) {
-    if (p.rows == kTileRows) hipLaunchKernelGGL((tile_kernel<D>), grid, block, 0, s, a);
+    if (p.rows == kTileRows) go(tile_kernel<D>, join_kernel<E, D, kTileRows>);
   }
-  if (p.n_split > 1)
-    hipLaunchKernelGGL((join_kernel<E, D>), dim3((unsigned)((long long)a.B * a.c.H_kv * a.T_max * a.G)), dim3(D / 4),
-                       0, s, a);
   return hipGetLastError();
 }
 
@@ -584,12 +760,17 @@ hipError_t launch(AttnArgs a, const AttnPlan& p, hipStream_t s) {
 
 AttnPlan attn_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtype, int d_head) {
   AttnPlan p;
+  const bool bf16 = dtype == TREVS_BF16;
   const long long n_rows = (long long)T_max * G;
-  p.rows = n_rows <= 16 || (d_head == 256 && dtype == TREVS_F32) ? 16 : n_rows <= 32 || dtype == TREVS_F32 ? 32 : kTileRows;
+  p.rows = n_rows <= 16 || (d_head == 256 && !bf16) ? 16 : n_rows <= 32 || !bf16 ? 32 : kTileRows;
   p.row_tiles = (int)((n_rows + p.rows - 1) / p.rows);
-  const long long wgs = (long long)B * H_kv * p.row_tiles, units = (kv_max + kUnit - 1) / kUnit;
-  const long long target = p.rows == kTileRows ? 1024 : 2048;
-  p.n_split = (int)std::max(1LL, std::min((target + wgs - 1) / wgs, (units + kWaves - 1) / kWaves));
+  const long long tiles = (long long)B * H_kv * p.row_tiles, steps = (kv_max + kStep - 1) / kStep;
+  // workgroups that run at once, and the steps that one takes side by side
+  const int per_cu = d_head == 256 || p.rows == 32 ? 1 : p.rows == 16 && bf16 ? 3 : 2;
+  const long long slots = 256LL * per_cu, side = p.rows == kTileRows ? 1 : kWaves;
+  // a tile to a workgroup while tiles are short or many; the steps of all must fit 31 bits to be cut
+  const bool cut = steps > 4 * side && tiles < 4 * slots && tiles * steps < INT32_MAX;
+  p.pieces = cut ? (int)std::min(slots, (tiles * steps + side - 1) / side) : 0;
   return p;
 }
 
