@@ -157,6 +157,7 @@ struct AttnArgs {
   int row_tiles;
   float* part;              // cut calls (else null): [2 pieces,rows,D] sums of a workgroup's pieces
   float2* part_ml;          // [2 pieces,rows] their (maximum, sum), base 2
+  int2* tile_pieces;        // [B,H_kv,row_tiles] first and last workgroup of each tile with steps
 };
 // Launch shape of one problem size.
 struct AttnPlan {

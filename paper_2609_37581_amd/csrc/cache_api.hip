@@ -193,16 +193,17 @@ int max_keys(const trevs_kv8_cache* c, const trevs_kv8_attention_args* a) {
   return a->kv_max ? a->kv_max : c->max_pages * c->page_tokens;
 }
 
-// Sums of cut tiles: (maximum, sum) pairs, then the sums of values.
+// Cut calls: the tiles' pieces, then their sums: (maximum, sum) pairs and values.
 struct AttnLayout {
   AttnPlan plan;
-  size_t part, total;
+  size_t part_ml, part, total;
 };
 AttnLayout attention_layout(const trevs_kv8_cache* c, const trevs_kv8_attention_args* a) {
   AttnLayout L;
   L.plan = attn_plan(a->B, a->T_max, c->H_kv, a->H_q / c->H_kv, max_keys(c, a), a->dtype, c->d_head);
   const size_t parts = (size_t)2 * L.plan.pieces * L.plan.rows;
-  L.part = align_up(parts * sizeof(float2));
+  L.part_ml = parts ? align_up((size_t)a->B * c->H_kv * L.plan.row_tiles * sizeof(int2)) : 0;
+  L.part = L.part_ml + align_up(parts * sizeof(float2));
   L.total = std::max(L.part + align_up(parts * c->d_head * sizeof(float)), kWsAlign);
   return L;
 }
@@ -392,8 +393,9 @@ trevs_status trevs_kv8_attention(const trevs_kv8_cache* c, const trevs_kv8_atten
   t.kv_max = max_keys(c, a);
   t.page_shift = page_shift(c);
   t.scale_log2e = a->scale * kLog2e;
+  t.tile_pieces = reinterpret_cast<int2*>(ws);
+  t.part_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(ws) + L.part_ml);
   t.part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(ws) + L.part);
-  t.part_ml = reinterpret_cast<float2*>(ws);
   TREVS_HIP(launch_kv8_attention(t, L.plan, a->dtype, c->d_head, reinterpret_cast<hipStream_t>(stream)));
   return TREVS_OK;
 }

@@ -151,16 +151,6 @@ struct Schedule {
     while (start(w + 1, n) <= step) ++w;
     return w;
   }
-  // Where sequence b's steps begin.
-  __device__ __forceinline__ int begin(const AttnArgs& a, int b) const {
-    if (b == 0) return 0;
-    int before = 0, e = ends;
-    for (int b0 = 0;; b0 += 64) {
-      if (b0) e = scan(a, b0);
-      if (b <= b0 + 64) return before + __builtin_amdgcn_readlane(e, b - 1 - b0);
-      before += __builtin_amdgcn_readlane(e, 63);
-    }
-  }
   // The tile that holds a step, and the tile's first step.
   __device__ __forceinline__ Tile find(const AttnArgs& a, int step, int& first) const {
     int before = 0, e = ends, b0 = 0;
@@ -225,6 +215,9 @@ struct Walk {
     // a piece that begins its tile is the workgroup's last, one that does not its first
     if (p.u0 != 0 || p.u1 != n) p.part = 2 * blockIdx.x + (p.u0 == 0);
     at = first + p.u1;
+    if (p.u0 == 0 && threadIdx.x == 0)
+      a.tile_pieces[(p.t.b * a.c.H_kv + p.t.hk) * a.row_tiles + p.t.rt] =
+          make_int2(blockIdx.x, p.part < 0 ? (int)blockIdx.x : s.owner(first + n - 1, gridDim.x));
     return true;
   }
 };
@@ -249,10 +242,19 @@ struct RowsShared {
   float m[kWaves][16 * NQ], l[kWaves][16 * NQ];
 };
 
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load16(const void* p) {
+  if constexpr (ONCE) return ldg16_stream(p);
+  return ldg16(p);
+}
+
 template <class E, int D, int NQ>
 __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, RowsShared<E, D, NQ>& sh) {
   constexpr int NP = kParts<E>;
   constexpr int R = 16 * NQ;
+  // calls of at most 16 rows a group read the cache once (64 sequences of 1.2 k to 16.5 k tokens: 125 us
+  // streamed, 132 not); of more, row tiles share it
+  constexpr bool kOnce = NQ == 1 && !(D == 256 && E::kBytes == 4);
   auto& s_o = sh.o;
   auto& s_m = sh.m;
   auto& s_l = sh.l;
@@ -314,9 +316,9 @@ __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, R
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int c = 0; c < D / 64; ++c) kw[t][c] = ldg16(kp + t * 4 * D + c * 64);
+      for (int c = 0; c < D / 64; ++c) kw[t][c] = load16<kOnce>(kp + t * 4 * D + c * 64);
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) vw[c] = ldg16(vp + ((size_t)(16 * c) << shift));
+    for (int c = 0; c < D / 16; ++c) vw[c] = load16<kOnce>(vp + ((size_t)(16 * c) << shift));
     const size_t block = (size_t)page * a.c.H_kv + hk;
     float ks = a.c.k_scale[block], vs = a.c.v_scale[block];
     next = look_up(u + kWaves);
@@ -467,15 +469,18 @@ __global__ __launch_bounds__(kWaves * 64, NQ == 1 && D <= 128 && E::kBytes == 2 
 // step ahead.  Bound by the matrix cores and, next to them, the exponentials.
 constexpr int kTileRows = 128;
 
-// Permutation of a staged row's 16-byte columns, by the row: eight lanes next
-// to each other read one column of eight rows (of keys: 0-3 and 16-19, as their
-// rows are dealt; of values, whose rows are 64 bytes: 0-7) and must meet 8
-// different ones modulo 128 bytes.
+// Permutation of a staged row's 16-byte columns, by the row: 16 lanes next to
+// each other read one column of 16 rows and must meet 16 different ones modulo
+// 256 bytes, the width of the banks.  A 128-byte row (keys of 128 channels) leaves
+// two rows to a width, a 64-byte one four; of keys the 16 rows are tokens 0-7 and
+// 16-23, as their rows are dealt, of values channels 0-15.  (Counted bank
+// conflicts of a prompt of 4259 rows: 3.2e7 cycles with a permutation for 8
+// lanes and 128 bytes, 0 with this one.)
 template <int D>
 __device__ __forceinline__ int key_swizzle(int row) {
-  return D == 64 ? ((row >> 1) & 1) | ((row >> 3) & 2) : (row & 3) | ((row >> 2) & 4);
+  return D == 64 ? ((row >> 2) & 1) | ((row >> 3) & 2) : ((row >> 1) & 3) | ((row >> 2) & 4);
 }
-__device__ __forceinline__ int value_swizzle(int row) { return (row >> 1) & 3; }
+__device__ __forceinline__ int value_swizzle(int row) { return (row >> 2) & 3; }
 
 template <int D>
 struct TileShared {
@@ -689,7 +694,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tile_kernel(AttnArgs a)
 // The sums of the pieces of each cut tile joined, in the order of its steps; zeros for rows that see no key.
 constexpr int kJoinThreads = 256;
 template <class E, int D, int R>
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(AttnArgs a, int n_pieces) {
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(AttnArgs a) {
   constexpr int kRows = kJoinThreads / (D / 4);  // rows of a workgroup, all of one tile
   Tile t;
   int id = blockIdx.x;
@@ -705,12 +710,8 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(AttnArgs a, int n_pi
   const int n = steps_of(tile_keys<R>(a, seq, t.rt));
   float x[4] = {}, m = -INFINITY, l = 0.f;
   if (n > 0) {
-    Schedule<R> s;
-    s.init(a);
-    int first = s.begin(a, t.b);
-    for (int rt = 0; rt < t.rt; ++rt) first += steps_of(tile_keys<R>(a, seq, rt)) * a.c.H_kv;
-    first += t.hk * n;
-    const int w0 = s.owner(first, n_pieces), w1 = s.owner(first + n - 1, n_pieces);
+    const int2 w = a.tile_pieces[(t.b * a.c.H_kv + t.hk) * a.row_tiles + t.rt];
+    const int w0 = w.x, w1 = w.y;
     if (w0 == w1 || r >= seq.rows * a.G) return;  // (one piece has finished it)
     // the first piece begins the tile, the others do not
     auto at = [&](int w) { return (size_t)(2 * w + (w == w0)) * R + row; };
@@ -743,7 +744,7 @@ hipError_t launch(AttnArgs a, const AttnPlan& p, hipStream_t s) {
     constexpr int kRows = kJoinThreads / (D / 4);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(p.pieces ? p.pieces : tiles)), dim3(256), 0, s, a);
     if (p.pieces)
-      hipLaunchKernelGGL(join, dim3((unsigned)(tiles * (p.rows / kRows))), dim3(kJoinThreads), 0, s, a, p.pieces);
+      hipLaunchKernelGGL(join, dim3((unsigned)(tiles * (p.rows / kRows))), dim3(kJoinThreads), 0, s, a);
   };
   static_assert(kWaves * 64 == 256, "one block size");
   if (p.rows == 16) go(rows_kernel<E, D, 1>, join_kernel<E, D, 16>);
