@@ -412,7 +412,8 @@ trevs_status trevs_kv8_compact(const trevs_kv8_cache* c, const trevs_kv8_compact
   t.K_in = a->K_in;
   t.n_kept = a->n_kept;
   t.n_layers = c->n_layers;
-  t.frames = c->max_pages;
+  // (a shorter source is skipped, a longer one there is none)
+  t.frames = (int)(((int64_t)c->max_pages * c->page_tokens - a->K_in + a->n_kept + c->page_tokens - 1) / c->page_tokens);
   TREVS_HIP(launch_kv8_compact(t, c->d_head, c->page_tokens, reinterpret_cast<hipStream_t>(stream)));
   return TREVS_OK;
 }
