@@ -104,13 +104,16 @@ __device__ __forceinline__ uint32_t free_bits(const PagesArgs& a, long long p) {
 __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(PagesArgs a, const int32_t* slots,
                                                                   const int32_t* n_new, int32_t* granted,
                                                                   int32_t* copy_src, int32_t* copy_dst) {
-  __shared__ int l_slot[kReserveThreads], l_last[kReserveThreads], l_off[kReserveThreads], l_col[kReserveThreads];
+  __shared__ __align__(16) int l_slot[kReserveThreads], l_last[kReserveThreads];
+  __shared__ int l_off[kReserveThreads + 1], l_col[kReserveThreads];
   __shared__ int l_need[kReserveThreads], l_ref[kReserveThreads], l_first[kReserveThreads], l_cow[kReserveThreads];
   __shared__ int red[kReserveThreads / 64];
   __shared__ unsigned long long l_sum;
   __shared__ int l_total;
-  const int i = threadIdx.x;
+  const int i = threadIdx.x, wave0 = i & ~63;
   const int max_tokens = a.max_pages << a.page_shift;
+  // the first pages' counts are on their way while the requests are read
+  const uint32_t bits0 = free_bits(a, 8 * i);
   int slot = -1, want_new = 0, len = 0;
   if (i < a.n) {
     slot = request_slot(a, slots, i);
@@ -121,8 +124,17 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(PagesArgs a, c
   if (i == 0) l_sum = 0;
   __syncthreads();
   bool ok = slot >= 0 && want_new >= 1 && want_new <= max_tokens - len;
-  if (slots)
-    for (int j = 0; j < i && ok; ++j) ok = l_slot[j] != slot;
+  // (waves without requests pass by the loops over the earlier ones; four entries a read)
+  const int4* slots4 = reinterpret_cast<const int4*>(l_slot);
+  if (slots && wave0 < a.n) {
+    bool same = false;
+    for (int j = 0; j < min(a.n, wave0 + 64); j += 4) {
+      const int4 x = slots4[j >> 2];
+      same = same || (j < i && x.x == slot) || (j + 1 < i && x.y == slot) || (j + 2 < i && x.z == slot) ||
+             (j + 3 < i && x.w == slot);
+    }
+    ok = ok && !same;
+  }
   // the last page, if rows would be appended to it
   const int have = pages_of(a, len), want = ok ? pages_of(a, (long long)len + want_new) : have;
   int last = -1;
@@ -136,21 +148,37 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(PagesArgs a, c
   __syncthreads();
   // of the requests that end in one shared page, each takes a copy until one holder is left
   int rank = 0, first = i;
-  if (last >= 0)
-    for (int j = i - 1; j >= 0; --j)
-      if (l_last[j] == last) ++rank, first = j;
+  const int4* last4 = reinterpret_cast<const int4*>(l_last);
+  if (__any(last >= 0)) {
+    auto earlier = [&](int j, int x) {
+      const bool same = j < i && last >= 0 && x == last;
+      rank += same;
+      first = same ? min(first, j) : first;
+    };
+    for (int j = 0; j < min(a.n, wave0 + 64); j += 4) {
+      const int4 x = last4[j >> 2];
+      earlier(j, x.x);
+      earlier(j + 1, x.y);
+      earlier(j + 2, x.z);
+      earlier(j + 3, x.w);
+    }
+  }
   bool cow = last >= 0 && rank < refs - 1;
   int need = ok ? want - have + cow : 0;
   l_need[i] = ok ? want - have : -1;  // without the copy; -1: refused already
   l_first[i] = first;
-  atomicAdd(&l_sum, (unsigned long long)need);
+  // all needs, which may pass 32 bits: their halves are summed by the wave, the waves' sums by 64-bit adds
+  // (one such add a thread took 3.8 us)
+  const uint32_t low = __builtin_amdgcn_readlane(wave_incl_scan(need & 0xffff, 0), 63);
+  const uint32_t high = __builtin_amdgcn_readlane(wave_incl_scan(need >> 16, 0), 63);
+  if ((i & 63) == 0 && (low | high)) atomicAdd(&l_sum, ((unsigned long long)high << 16) + low);
   __syncthreads();
   const unsigned long long sum = l_sum;
   // free pages, until they cover the requests
   long long n_free = 0;
   for (long long p0 = 0; p0 < a.n_pages && (unsigned long long)n_free < sum; p0 += 8 * kReserveThreads) {
     int total;
-    block_excl_scan(__popc(free_bits(a, p0 + 8 * i)), red, total);
+    block_excl_scan(__popc(p0 ? free_bits(a, p0 + 8 * i) : bits0), red, total);
     n_free += total;
   }
   if (sum > (unsigned long long)n_free) {
@@ -181,34 +209,37 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(PagesArgs a, c
     cow = ok && l_last[i] >= 0;
     need = ok ? l_need[i] + cow : 0;
     if (i >= a.n) l_off[i] = l_total;
+    if (i == 0) l_off[kReserveThreads] = l_total;
   } else {
     int total;
     l_off[i] = block_excl_scan(need, red, total);
-    l_total = total;
+    if (i == 0) l_off[kReserveThreads] = l_total = total;
   }
   l_cow[i] = cow;
   l_col[i] = have - cow;
   __syncthreads();
   const int total = l_total;
+  const int reach = a.n > 1 ? 1 << (31 - __builtin_clz(a.n - 1)) : 0;  // largest power of two below n
   // the r-th lowest free page goes to the request whose range holds r
   int base = 0;
   for (long long p0 = 0; p0 < a.n_pages && base < total; p0 += 8 * kReserveThreads) {
     const long long p = p0 + 8 * i;
-    uint32_t bits = free_bits(a, p);
+    uint32_t bits = p0 ? free_bits(a, p) : bits0;
     int sum_step;
     int r = base + block_excl_scan(__popc(bits), red, sum_step);
     base += sum_step;
-    while (bits && r < total) {
-      const int k = __builtin_ctz(bits);
-      bits &= bits - 1;
-      int at = 0;
-#pragma unroll
-      for (int step = kReserveThreads / 2; step > 0; step >>= 1) at += l_off[at + step] <= r ? step : 0;
-      const int o = r - l_off[at];
-      a.table[(size_t)l_slot[at] * a.max_pages + l_col[at] + o] = (int)(p + k);
-      a.ref[p + k] = 1;
-      if (o == 0 && l_cow[at]) copy_dst[at] = (int)(p + k);
-      ++r;
+    if (bits && r < total) {
+      int at = 0;  // the last request whose range begins at or before r
+      for (int step = reach; step > 0; step >>= 1) at += l_off[at + step] <= r ? step : 0;
+      while (bits && r < total) {
+        while (l_off[at + 1] <= r) ++at;  // (l_off[n] = total)
+        const int k = __builtin_ctz(bits), o = r - l_off[at];
+        bits &= bits - 1;
+        a.table[(size_t)l_slot[at] * a.max_pages + l_col[at] + o] = (int)(p + k);
+        a.ref[p + k] = 1;
+        if (o == 0 && l_cow[at]) copy_dst[at] = (int)(p + k);
+        ++r;
+      }
     }
   }
   if (i >= a.n) return;
