@@ -265,6 +265,17 @@ __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, R
   const int rows = seq.rows, slot = seq.slot, L = seq.L, n_rows = rows * a.G;
   const int n_keys = tile_keys<R>(a, seq, pc.t.rt);
 
+  // A lane looks up the page of its 16 tokens (weights, values) a unit ahead; its key rows, of tile t
+  // row 4 y + i = token 16 y + 4 t + i, lie in the page of lane group y.  Their places in a page are the
+  // same in every unit (64 tokens are whole pages).
+  const int shift = a.page_shift, page_mask = (1 << shift) - 1;
+  const size_t page_stride = ((size_t)D << shift) * a.c.H_kv;
+  const int key_row = (16 * (n16 >> 2) & page_mask) + (n16 & 3);
+  const uint8_t* k_base = a.c.k + ((size_t)hk * D << shift) + key_row * D + 16 * g4;
+  const uint8_t* v_base = a.c.v + ((size_t)hk * D << shift) + ((size_t)n16 << shift) + (16 * g4 & page_mask);
+  const int32_t* table = a.c.table + (size_t)max(slot, 0) * a.c.max_pages;
+  auto look_up = [&](int u) { return table[min((u * kStep + 16 * g4) >> shift, a.c.max_pages - 1)]; };
+  int next = slot >= 0 ? look_up(u0 + wave) : -1;  // (not held up by the length)
   int lim[NQ];  // keys that this lane's query row sees
   bf16x8 q[NQ][D / 32][NP];
 #pragma unroll
@@ -294,18 +305,6 @@ __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, R
     for (int c = 0; c < D / 16; ++c) o[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // A lane looks up the page of its 16 tokens (weights, values) a unit ahead; its key rows, of tile t
-  // row 4 y + i = token 16 y + 4 t + i, lie in the page of lane group y.  Their places in a page are the
-  // same in every unit (64 tokens are whole pages).
-  const int shift = a.page_shift, page_mask = (1 << shift) - 1;
-  const size_t page_stride = ((size_t)D << shift) * a.c.H_kv;
-  const int key_row = (16 * (n16 >> 2) & page_mask) + (n16 & 3);
-  const uint8_t* k_base = a.c.k + ((size_t)hk * D << shift) + key_row * D + 16 * g4;
-  const uint8_t* v_base = a.c.v + ((size_t)hk * D << shift) + ((size_t)n16 << shift) + (16 * g4 & page_mask);
-  const int32_t* table = a.c.table + (size_t)max(slot, 0) * a.c.max_pages;
-  const int last_page = max(n_keys - 1, 0) >> shift;
-  auto look_up = [&](int u) { return table[min((u * kStep + 16 * g4) >> shift, last_page)]; };
-  int next = u0 + wave < u1 ? look_up(u0 + wave) : -1;
   for (int u = u0 + wave; u < u1; u += kWaves) {
     const int tok = u * kStep + 16 * g4;
     const bool there = next >= 0 && next < a.c.n_pages && tok < n_keys;
