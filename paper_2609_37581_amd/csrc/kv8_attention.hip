@@ -99,7 +99,9 @@ constexpr int kStep = 64;  // tokens of a step
 // that its last row sees.  Calls of few tiles, or of uneven ones, cut the
 // steps of all of them, one after the other (sequences, row tiles, groups),
 // into gridDim.x equal pieces, a workgroup to a piece: a piece that covers a
-// tile finishes it, the others leave their sums to join_kernel.
+// tile finishes it, the others leave their sums to join_kernel.  (8 questions
+// over 16.5 k tokens: 225 us; groups before row tiles 238, the same with
+// neighbouring pieces on one XCD.)
 struct Tile {
   int b, hk, rt;
 };
@@ -151,50 +153,65 @@ struct Schedule {
     while (start(w + 1, n) <= step) ++w;
     return w;
   }
-  // The tile that holds a step, and the tile's first step.
-  __device__ __forceinline__ Tile find(const AttnArgs& a, int step, int& first) const {
-    int before = 0, e = ends, b0 = 0;
-    while (before + __builtin_amdgcn_readlane(e, 63) <= step) {
-      before += __builtin_amdgcn_readlane(e, 63);
-      b0 += 64;
-      e = scan(a, b0);
-    }
-    const int i = __builtin_ctzll(__ballot(before + e > step));
-    Tile t;
-    t.b = b0 + i;
-    first = before + (i ? __builtin_amdgcn_readlane(e, i - 1) : 0);
-    const Sequence s = sequence(a, t.b);
-    for (t.rt = 0;; ++t.rt) {
-      const int n = steps_of(tile_keys<R>(a, s, t.rt));
-      if (step < first + n * a.c.H_kv) {
-        t.hk = (step - first) / n;
-        first += t.hk * n;
-        return t;
-      }
-      first += n * a.c.H_kv;
-    }
-  }
 };
 
 // A workgroup's way through its work: in a cut call the pieces of tiles that its steps cover, else one tile.
 struct Piece {
   Tile t;
+  Sequence seq;
   int u0, u1;   // steps of the tile
   int part;     // -1: the whole tile; else where its sums go
 };
 template <int R>
 struct Walk {
   Schedule<R> s;
-  int at, end;
+  int at, end;         // steps still to do
+  Tile t;              // the tile that `at` lies in,
+  Sequence seq;        // its sequence,
+  int first, n;        // its first step and its steps
   __device__ __forceinline__ explicit Walk(const AttnArgs& a) : at(0), end(1) {
     if (!a.part) return;
     s.init(a);
     at = s.start(blockIdx.x, gridDim.x);
     end = s.start(blockIdx.x + 1, gridDim.x);
+    if (at < end) locate(a);
+  }
+  __device__ __forceinline__ void locate(const AttnArgs& a) {
+    int before = 0, e = s.ends, b0 = 0;
+    while (before + __builtin_amdgcn_readlane(e, 63) <= at) {
+      before += __builtin_amdgcn_readlane(e, 63);
+      b0 += 64;
+      e = s.scan(a, b0);
+    }
+    const int i = __builtin_ctzll(__ballot(before + e > at));
+    t.b = b0 + i;
+    first = before + (i ? __builtin_amdgcn_readlane(e, i - 1) : 0);
+    seq = sequence(a, t.b);
+    for (t.rt = 0;; ++t.rt) {
+      n = steps_of(tile_keys<R>(a, seq, t.rt));
+      if (at < first + n * a.c.H_kv) break;
+      first += n * a.c.H_kv;
+    }
+    t.hk = (at - first) / n;
+    first += t.hk * n;
+  }
+  // To the next tile that has steps (there is one: at < end).
+  __device__ __forceinline__ void advance(const AttnArgs& a) {
+    first += n;
+    if (++t.hk < a.c.H_kv) return;
+    t.hk = 0;
+    do {
+      if (++t.rt * R >= seq.rows * a.G) {
+        t.rt = 0;
+        seq = sequence(a, ++t.b);
+      }
+      n = steps_of(tile_keys<R>(a, seq, t.rt));
+    } while (n == 0);
   }
   __device__ __forceinline__ bool next(const AttnArgs& a, Piece& p) {
     if (at >= end) return false;
     p.part = -1;
+    p.u0 = 0;
     if (!a.part) {
       // not cut: groups (b, hk) next to each other, so that a group's tiles meet on the XCDs that share
       // its index modulo 8; the tiles with the most keys first
@@ -202,22 +219,22 @@ struct Walk {
       p.t.rt = a.row_tiles - 1 - blockIdx.x / groups;
       p.t.b = group / a.c.H_kv;
       p.t.hk = group - p.t.b * a.c.H_kv;
-      p.u0 = 0;
-      p.u1 = steps_of(tile_keys<R>(a, sequence(a, p.t.b), p.t.rt));
+      p.seq = sequence(a, p.t.b);
+      p.u1 = steps_of(tile_keys<R>(a, p.seq, p.t.rt));
       at = end;
       return true;
     }
-    int first;
-    p.t = s.find(a, at, first);
-    const int n = steps_of(tile_keys<R>(a, sequence(a, p.t.b), p.t.rt));
+    p.t = t;
+    p.seq = seq;
     p.u0 = at - first;
     p.u1 = min(n, end - first);
     // a piece that begins its tile is the workgroup's last, one that does not its first
     if (p.u0 != 0 || p.u1 != n) p.part = 2 * blockIdx.x + (p.u0 == 0);
-    at = first + p.u1;
     if (p.u0 == 0 && threadIdx.x == 0)
-      a.tile_pieces[(p.t.b * a.c.H_kv + p.t.hk) * a.row_tiles + p.t.rt] =
+      a.tile_pieces[(t.b * a.c.H_kv + t.hk) * a.row_tiles + t.rt] =
           make_int2(blockIdx.x, p.part < 0 ? (int)blockIdx.x : s.owner(first + n - 1, gridDim.x));
+    at = first + p.u1;
+    if (at < end) advance(a);
     return true;
   }
 };
@@ -261,7 +278,7 @@ __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, R
   const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int b = pc.t.b, hk = pc.t.hk, r0 = pc.t.rt * R, u0 = pc.u0, u1 = pc.u1;
-  const Sequence seq = sequence(a, b);
+  const Sequence& seq = pc.seq;
   const int rows = seq.rows, slot = seq.slot, L = seq.L, n_rows = rows * a.G;
   const int n_keys = tile_keys<R>(a, seq, pc.t.rt);
 
@@ -498,7 +515,7 @@ __device__ __forceinline__ void tile_piece(const AttnArgs& a, const Piece& pc, T
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int b = pc.t.b, hk = pc.t.hk, r0 = pc.t.rt * kTileRows, u0 = pc.u0, u1 = pc.u1;
-  const Sequence seq = sequence(a, b);
+  const Sequence& seq = pc.seq;
   const int rows = seq.rows, slot = seq.slot, L = seq.L, n_rows = rows * a.G;
   const int n_keys = tile_keys<kTileRows>(a, seq, pc.t.rt);
 
@@ -690,47 +707,64 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tile_kernel(AttnArgs a)
   while (walk.next(a, p)) tile_piece<D>(a, p, sh);  // (a piece ends with its last reads of LDS behind a barrier)
 }
 
-// The sums of the pieces of each cut tile joined, in the order of its steps; zeros for rows that see no key.
+// The sums of the pieces of each cut tile joined, in the order of its steps;
+// zeros for rows that see no key.  D / 4 threads hold a row, four channels
+// each; tiles of many pieces (MANY: 8 or more on average) give a row to a whole
+// workgroup, each D / 4 threads to every kJoinThreads / (D / 4)-th piece (one
+// sequence of 16 k tokens, 64 pieces a tile: 46.6 us without, @@ with).
 constexpr int kJoinThreads = 256;
-template <class E, int D, int R>
+template <class E, int D, int R, bool MANY>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(AttnArgs a) {
-  constexpr int kRows = kJoinThreads / (D / 4);  // rows of a workgroup, all of one tile
+  constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes, kRows = MANY ? 1 : kGroups;
+  __shared__ float4 s_x[MANY ? kGroups : 1][kLanes];
+  __shared__ float s_l[MANY ? kGroups : 1];
+  const int group = threadIdx.x / kLanes, c = threadIdx.x % kLanes * 4;
   Tile t;
   int id = blockIdx.x;
-  const int sub = id % (R / kRows);
+  const int row = id % (R / kRows) * kRows + (MANY ? 0 : group);
   id /= R / kRows;
   t.rt = id % a.row_tiles;
   id /= a.row_tiles;
   t.b = id / a.c.H_kv;
   t.hk = id - t.b * a.c.H_kv;
   const Sequence seq = sequence(a, t.b);
-  const int row = sub * kRows + threadIdx.x / (D / 4), r = t.rt * R + row, c = threadIdx.x % (D / 4) * 4;
-  if (t.rt * R + sub * kRows >= seq.rows * a.G) return;
-  const int n = steps_of(tile_keys<R>(a, seq, t.rt));
-  float x[4] = {}, m = -INFINITY, l = 0.f;
-  if (n > 0) {
-    const int2 w = a.tile_pieces[(t.b * a.c.H_kv + t.hk) * a.row_tiles + t.rt];
-    const int w0 = w.x, w1 = w.y;
-    if (w0 == w1 || r >= seq.rows * a.G) return;  // (one piece has finished it)
+  const int r = t.rt * R + row;
+  if (r >= seq.rows * a.G) return;  // (one row or whole groups of lanes: no barrier is missed)
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  float m = -INFINITY, l = 0.f;
+  if (tile_keys<R>(a, seq, t.rt) > 0) {
+    const int2 pieces = a.tile_pieces[(t.b * a.c.H_kv + t.hk) * a.row_tiles + t.rt];
+    const int w0 = pieces.x, n = pieces.y - pieces.x + 1;
+    if (n == 1) return;  // (one piece has finished it)
     // the first piece begins the tile, the others do not
-    auto at = [&](int w) { return (size_t)(2 * w + (w == w0)) * R + row; };
-    for (int w = w0; w <= w1; ++w) m = fmaxf(m, a.part_ml[at(w)].x);
-    for (int w = w0; w <= w1; ++w) {
-      const float2 ml = a.part_ml[at(w)];
+    auto at = [&](int i) { return (size_t)(2 * (w0 + i) + (i == 0)) * R + row; };
+    for (int i = threadIdx.x % kLanes; i < n; i += kLanes) m = fmaxf(m, a.part_ml[at(i)].x);
+#pragma unroll
+    for (int d = 1; d < kLanes; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+#pragma unroll 4
+    for (int i = MANY ? group : 0; i < n; i += MANY ? kGroups : 1) {
+      const float2 ml = a.part_ml[at(i)];
+      const float4 y = *reinterpret_cast<const float4*>(a.part + at(i) * D + c);
       const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
       l = fmaf(ml.y, f, l);
-      const float4 y = *reinterpret_cast<const float4*>(a.part + at(w) * D + c);
-      x[0] = fmaf(y.x, f, x[0]);
-      x[1] = fmaf(y.y, f, x[1]);
-      x[2] = fmaf(y.z, f, x[2]);
-      x[3] = fmaf(y.w, f, x[3]);
+      x = make_float4(fmaf(y.x, f, x.x), fmaf(y.y, f, x.y), fmaf(y.z, f, x.z), fmaf(y.w, f, x.w));
+    }
+    if constexpr (MANY) {
+      s_x[group][c / 4] = x;
+      if (c == 0) s_l[group] = l;
+      __syncthreads();
+      if (group) return;
+      for (int g = 1; g < kGroups; ++g) {
+        const float4 y = s_x[g][c / 4];
+        x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+        l += s_l[g];
+      }
     }
   }
-  if (r >= seq.rows * a.G) return;
+  if (MANY && group) return;
   const float inv = l > 0.f ? 1.f / l : 0.f;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) x[j] *= inv;
-  store4(a.out, out_row(a, t, r) * D + c, x, E());
+  const float out[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
+  store4(a.out, out_row(a, t, r) * D + c, out, E());
   if (a.lse && c == 0) store_lse(a, t, r, m, l);
 }
 
@@ -739,19 +773,23 @@ hipError_t launch(AttnArgs a, const AttnPlan& p, hipStream_t s) {
   a.row_tiles = p.row_tiles;
   if (p.pieces == 0) a.part = nullptr;
   const long long tiles = (long long)a.B * a.c.H_kv * p.row_tiles;
-  auto go = [&](auto kernel, auto join) {
-    constexpr int kRows = kJoinThreads / (D / 4);
+  const bool many = p.pieces >= 8 * tiles;
+  auto go = [&](auto kernel, auto join, auto join_many) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)(p.pieces ? p.pieces : tiles)), dim3(256), 0, s, a);
-    if (p.pieces)
-      hipLaunchKernelGGL(join, dim3((unsigned)(tiles * (p.rows / kRows))), dim3(kJoinThreads), 0, s, a);
+    if (!p.pieces) return;
+    const long long rows = tiles * p.rows;
+    if (many)
+      hipLaunchKernelGGL(join_many, dim3((unsigned)rows), dim3(kJoinThreads), 0, s, a);
+    else
+      hipLaunchKernelGGL(join, dim3((unsigned)(rows / (kJoinThreads / (D / 4)))), dim3(kJoinThreads), 0, s, a);
   };
   static_assert(kWaves * 64 == 256, "one block size");
-  if (p.rows == 16) go(rows_kernel<E, D, 1>, join_kernel<E, D, 16>);
+  if (p.rows == 16) go(rows_kernel<E, D, 1>, join_kernel<E, D, 16, false>, join_kernel<E, D, 16, true>);
   if constexpr (!(D == 256 && E::kBytes == 4)) {
-    if (p.rows == 32) go(rows_kernel<E, D, 2>, join_kernel<E, D, 32>);
+    if (p.rows == 32) go(rows_kernel<E, D, 2>, join_kernel<E, D, 32, false>, join_kernel<E, D, 32, true>);
   }
   if constexpr (E::kBytes == 2) {
-    if (p.rows == kTileRows) go(tile_kernel<D>, join_kernel<E, D, kTileRows>);
+    if (p.rows == kTileRows) go(tile_kernel<D>, join_kernel<E, D, kTileRows, false>, join_kernel<E, D, kTileRows, true>);
   }
   return hipGetLastError();
 }
@@ -768,8 +806,16 @@ AttnPlan attn_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtype, int
   // workgroups that run at once, and the steps that one takes side by side
   const int per_cu = d_head == 256 || p.rows == 32 ? 1 : p.rows == 16 && bf16 ? 3 : 2;
   const long long slots = 256LL * per_cu, side = p.rows == kTileRows ? 1 : kWaves;
-  // a tile to a workgroup while tiles are short or many; the steps of all must fit 31 bits to be cut
-  const bool cut = steps > 4 * side && tiles < 4 * slots && tiles * steps < INT32_MAX;
+  // Uncut, the last round of workgroups leaves `idle` slots without a tile for as long as a tile takes
+  // (a step of a workgroup: about 1.5 us, 3 in fp32); cut, a second launch joins the pieces and each piece
+  // begins anew, about 10 us.  Measured, uncut / cut: one token of 64 sequences of 1.2 k to 16.5 k tokens,
+  // 256 tiles for 768 slots, 210 / 115 us; of 32 sequences of 4000 with 16 heads of 64, 512 tiles, 45 / 54;
+  // prompts of 4 x 2048 with 16 heads of 64, 1024 tiles for 512 slots, 65 / 154.  Calls of two rounds or more
+  // are not cut: their long tiles go first, and tiles of a group that run at once share its keys in the L2,
+  // which pieces do not (prompts of 4259 rows, 3728 tiles for 512 slots: 590 / 1085).
+  // The steps of all must fit 31 bits.
+  const long long idle = (tiles + slots - 1) / slots * slots - tiles;
+  const bool cut = tiles < 2 * slots && idle * (steps / side) * (bf16 ? 3 : 6) > 20 * slots && tiles * steps < INT32_MAX;
   p.pieces = cut ? (int)std::min(slots, (tiles * steps + side - 1) / side) : 0;
   return p;
 }
