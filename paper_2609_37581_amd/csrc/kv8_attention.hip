@@ -298,7 +298,8 @@ __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, R
 #pragma unroll
   for (int i = 0; i < NQ; ++i) {
     const int r = r0 + 16 * i + n16, t = r / a.G, g = r - t * a.G;
-    lim[i] = r < n_rows ? (a.causal ? min(L - rows + t + 1, L) : L) : 0;
+    // (a row past the last is not stored: it need not be masked)
+    lim[i] = r < n_rows ? (a.causal ? min(L - rows + t + 1, L) : L) : n_keys;
     const size_t at = ((size_t)b * a.T_max + t) * a.q_ld + (size_t)(hk * a.G + g) * D;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
@@ -522,7 +523,7 @@ __device__ __forceinline__ void tile_piece(const AttnArgs& a, const Piece& pc, T
   // this lane's query row: half h holds channels 32 (c/2) + 16 h + 8 (c%2) .. +7, as the keys' 16-byte reads give them
   const int r = r0 + 32 * wave + col, t = r / a.G, g = r - t * a.G;
   const bool live = r < n_rows;
-  const int lim = live ? (a.causal ? min(L - rows + t + 1, L) : L) : 0;
+  const int lim = live ? (a.causal ? min(L - rows + t + 1, L) : L) : n_keys;
   bf16x8 q[D / 16];
   {
     const size_t at = ((size_t)b * a.T_max + t) * a.q_ld + (size_t)(hk * a.G + g) * D + 16 * half;
@@ -531,9 +532,10 @@ __device__ __forceinline__ void tile_piece(const AttnArgs& a, const Piece& pc, T
       q[c] = __builtin_bit_cast(
           bf16x8, live ? ldg16(reinterpret_cast<const uint16_t*>(a.q) + at + c / 2 * 32 + 8 * (c & 1)) : zero4());
   }
-  // keys every row of the wave sees
+  // keys that every row of the wave sees (a row past the last is not stored: it need not be masked)
   const int w_first = r0 + 32 * wave;
-  const int lim_all = w_first + 31 < n_rows ? (a.causal ? min(L - rows + w_first / a.G + 1, L) : L) : 0;
+  const int lim_all = a.causal ? min(L - rows + w_first / a.G + 1, L) : L;
+  const bool busy = w_first < n_rows;  // a wave without rows only stages
 
   f32x16 o[D / 32];
 #pragma unroll
@@ -605,70 +607,72 @@ __device__ __forceinline__ void tile_piece(const AttnArgs& a, const Piece& pc, T
     // (past the last step: its own pages again, not used)
     load(u + 1);
     look_up(u + 2);
-    f32x16 s[2];
-    float ks[2];
+    if (busy) {
+      f32x16 s[2];
+      float ks[2];
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      ks[y] = s_ks[buf][2 * y + half];
+      for (int y = 0; y < 2; ++y) {
+        ks[y] = s_ks[buf][2 * y + half];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
-      // row 8j + 4h + i of the product is token 16 h + 4 j + i
-      const int kr = 32 * y + 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);
+        for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
+        // row 8j + 4h + i of the product is token 16 h + 4 j + i
+        const int kr = 32 * y + 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) {
-        const u32x4 w = s_k[buf][kr * (D / 16) + ((2 * c + half) ^ key_swizzle<D>(kr))];
-        s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(w[0], w[1], 1.f), q[2 * c], s[y], 0, 0, 0);
-        s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(w[2], w[3], 1.f), q[2 * c + 1], s[y], 0, 0, 0);
+        for (int c = 0; c < D / 32; ++c) {
+          const u32x4 w = s_k[buf][kr * (D / 16) + ((2 * c + half) ^ key_swizzle<D>(kr))];
+          s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(w[0], w[1], 1.f), q[2 * c], s[y], 0, 0, 0);
+          s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(w[2], w[3], 1.f), q[2 * c + 1], s[y], 0, 0, 0);
+        }
       }
-    }
-    const bool whole = (u + 1) * kStep <= lim_all && __all(ks[0] >= 0.f && ks[1] >= 0.f);
-    float f[2];
+      const bool whole = (u + 1) * kStep <= lim_all && __all(ks[0] >= 0.f && ks[1] >= 0.f);
+      float f[2];
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      f[y] = fabsf(ks[y]) * a.scale_log2e;
-      if (!whole) {
-        const int n = ks[y] >= 0.f ? lim - (u * kStep + 32 * y + 16 * half) : 0;
+      for (int y = 0; y < 2; ++y) {
+        f[y] = fmaxf(fabsf(ks[y]) * a.scale_log2e, 0x1p-126f);  // (never 0: the masked -inf stay what they are)
+        if (!whole) {
+          const int n = ks[y] >= 0.f ? lim - (u * kStep + 32 * y + 16 * half) : 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[y][i] = i < n ? s[y][i] : -INFINITY;
+          for (int i = 0; i < 16; ++i) s[y][i] = i < n ? s[y][i] : -INFINITY;
+        }
       }
-    }
-    float top = -INFINITY;
+      float top = -INFINITY;
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      float x = s[y][0];
+      for (int y = 0; y < 2; ++y) {
+        float x = s[y][0];
 #pragma unroll
-      for (int i = 1; i < 16; ++i) x = fmaxf(x, s[y][i]);
-      top = fmaxf(top, x * f[y]);
-    }
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    if (__any(top > m + kSlack)) {
-      const float now = fmaxf(top, m), old = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
-      m = now;
-      l *= old;
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[c][i] *= old;
-    }
-    const float base = m == -INFINITY ? 0.f : m;
-    bf16x8 p[4];
-#pragma unroll
-    for (int y = 0; y < 2; ++y)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[y][i], f[y], -base));
-        l += x;
-        p[2 * y + (i >> 3)][i & 7] = (__bf16)x;
+        for (int i = 1; i < 16; ++i) x = fmaxf(x, s[y][i]);
+        top = fmaxf(top, x * f[y]);
       }
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      if (__any(top > m + kSlack)) {
+        const float now = fmaxf(top, m), old = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
+        m = now;
+        l *= old;
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      const float vs = s_vs[buf][2 * y + half];
+        for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) {
-        const int vr = 32 * c + col;
-        const u32x4 w = s_v[buf][vr * 4 + ((2 * y + half) ^ value_swizzle(vr))];
-        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(w[0], w[1], vs), p[2 * y], o[c], 0, 0, 0);
-        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(w[2], w[3], vs), p[2 * y + 1], o[c], 0, 0, 0);
+          for (int i = 0; i < 16; ++i) o[c][i] *= old;
+      }
+      const float base = m == -INFINITY ? 0.f : m;
+      bf16x8 p[4];
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(s[y][i], f[y], -base));
+          l += x;
+          p[2 * y + (i >> 3)][i & 7] = (__bf16)x;
+        }
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const float vs = s_vs[buf][2 * y + half];
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          const int vr = 32 * c + col;
+          const u32x4 w = s_v[buf][vr * 4 + ((2 * y + half) ^ value_swizzle(vr))];
+          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(w[0], w[1], vs), p[2 * y], o[c], 0, 0, 0);
+          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(w[2], w[3], vs), p[2 * y + 1], o[c], 0, 0, 0);
+        }
       }
     }
     store(buf ^ 1);

@@ -628,6 +628,8 @@ class Rope:
                  attn_factor=1.0, inplace=False):
         self.device = dev = q.device
         dt = q.dtype
+        if dev.type != "cuda":
+            raise ValueError("q must be on a GPU")
         a = RopeArgs()
         a.struct_size = ctypes.sizeof(RopeArgs)
         a.dtype = _dtype_code(q)
@@ -683,7 +685,9 @@ class Kv8Cache:
     def __init__(self, *, n_pages, page_tokens, n_slots, max_pages, H_kv, d_head, n_layers=1,
                  device="cuda"):
         dev = torch.device(device)
-        if dev.type == "cuda" and dev.index is None:
+        if dev.type != "cuda":
+            raise ValueError("the cache lives on a GPU")
+        if dev.index is None:
             dev = torch.device("cuda", torch.cuda.current_device())
         if min(n_pages, page_tokens, n_slots, max_pages, H_kv, d_head, n_layers) < 1:
             raise ValueError("every size of a cache is at least 1")

@@ -338,6 +338,48 @@ def test_attention_long_and_layers(T):
     assert torch.equal(first, again)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,H_q,H_kv,causal", [(1, 2, 1, True), (1, 40, 2, True), (3, 14, 2, True), (9, 8, 2, False),
+                                               (40, 8, 2, True)])
+def test_attention_of_many_uneven_sequences(T, H_q, H_kv, causal, dtype):
+    """More than 64 sequences, empty ones and questions of no row among them, in
+    calls that are cut into pieces: a wave's scan of the sequences goes on past
+    its lanes, pieces cover tiles in part, whole and several."""
+    print(f"[attn uneven] {T} {H_q} {H_kv} {causal} {dtype}", flush=True)
+    rng = np.random.default_rng(T)
+    B = 140 if T < 9 else 70
+    lens = [int(n) for n in rng.integers(0, 90, B)]
+    for i in (0, 5, 63, 64, 65, B - 1):
+        lens[i] = int(rng.integers(200, 400))
+    lens[7] = lens[66] = 0
+    m = model(rng, lens, 16, H_kv, 64)
+    m.max_pages = 256  # (a longer table: the call is planned for what it could hold)
+    m.table = [row + [-1] * (256 - len(row)) for row in m.table]
+    c = device_cache(m)
+    q, qs = storage(rng.normal(size=(B, T, H_q, 64)), dtype)
+    q_len = rng.integers(0, T + 1, B).tolist()
+    run_attention(m, c, q, qs, dtype, q_len=q_len, causal=causal)
+    run_attention(m, c, q, qs, dtype, q_len=[0] * B, causal=causal)  # no work at all
+
+
+@pytest.mark.parametrize("T", [1, 50])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_attention_scales_at_their_ends(T, dtype):
+    """Blocks whose scales lie far apart, zero blocks with the smallest scale,
+    and a logit scale so small that its product with that is no float."""
+    rng = np.random.default_rng(13)
+    m = model(rng, [200, 97], 16, 2, 64)
+    m.v_scale *= np.exp2(rng.integers(-40, 41, m.v_scale.shape))
+    m.k_scale *= np.exp2(rng.integers(-30, 1, m.k_scale.shape))
+    for p in (m.table[0][2], m.table[1][0]):
+        m.k[0, p] = m.v[0, p] = 0.0
+        m.k_scale[0, p] = m.v_scale[0, p] = 2.0 ** -126
+    c = device_cache(m)
+    q, qs = storage(rng.normal(size=(2, T, 4, 64)), dtype)
+    run_attention(m, c, q, qs, dtype)
+    run_attention(m, c, q, qs, dtype, scale=1e-12)
+
+
 def test_offsets_past_32_bits():
     """Pages whose bytes lie past 4 GiB: written, read, copied and compacted."""
     page, H, d, n_pages = 64, 32, 256, 8300  # 512 KiB a page and side, 4.3 GB
