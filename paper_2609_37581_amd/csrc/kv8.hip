@@ -170,15 +170,16 @@ __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void write_kernel(Write
 // A destination block's tokens: source block and place of each, -1 for none.
 template <int PAGE>
 struct TokenMap {
-  int block[PAGE], at[PAGE];
+  int block[PAGE];
   float scale[PAGE];
+  u32x4 at[PAGE / 16];  // a byte a token
 };
 
 // Block (layer, b, f, h) of a destination, gathered from the source's rows.
 // Values lie token last, a byte of each channel apart: a workgroup brings each
 // source block that its tokens name into LDS whole, 16 bytes a lane, and takes
 // the bytes from there (single bytes from memory, a line each: 37.5 us for 4
-// layers of 4 x 1187 of 4259 tokens, this way 24).
+// layers of 4 x 1187 of 4259 tokens, this way 20).
 template <int D, int PAGE>
 __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void compact_kernel(CompactArgs a) {
   using B = Block<D, PAGE>;
@@ -213,7 +214,7 @@ __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void compact_kernel(Com
   if (tid < 64) {
     if (tid < PAGE) {
       map.block[tid] = from;
-      map.at[tid] = at;
+      reinterpret_cast<uint8_t*>(map.at)[tid] = (uint8_t)at;
       map.scale[tid] = from >= 0 ? scales[(size_t)from * a.c.H_kv] : 0.f;
     }
     const int before = __shfl_up(from, 1, 64);
@@ -233,7 +234,7 @@ __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void compact_kernel(Com
         const int t = t0 + i;
         const int from = t < hi ? map.block[t] : -1;
         const u32x2 w = from >= 0 ? *reinterpret_cast<const u32x2*>(data + (size_t)from * a.c.H_kv * (PAGE * D) +
-                                                                    map.at[t] * D + c)
+                                                                    reinterpret_cast<const uint8_t*>(map.at)[t] * D + c)
                                   : u32x2{0u, 0u};
         float y[2][4];
         from_e4m3(w[0], y[0]);
@@ -254,7 +255,7 @@ __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void compact_kernel(Com
   // a thread's items: 16 tokens of a channel, as bytes
   constexpr int kGroups = PAGE / 16, kItems = D * kGroups / B::kThreads;
   static_assert(kItems * B::kThreads == D * kGroups, "whole items");
-  u32x4 w[kItems], next[kItems];
+  u32x4 w[kItems], next[kItems], at16[kItems];
   uint64_t runs = s_runs;
   auto fetch = [&](int t) {
     const int from = map.block[t];
@@ -263,7 +264,10 @@ __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void compact_kernel(Com
       next[i] = from >= 0 ? ldg16(data + (size_t)from * a.c.H_kv * (PAGE * D) + (tid + i * B::kThreads) * 16) : zero4();
   };
 #pragma unroll
-  for (int i = 0; i < kItems; ++i) w[i] = zero4();
+  for (int i = 0; i < kItems; ++i) {
+    w[i] = zero4();
+    at16[i] = map.at[(tid + i * B::kThreads) % kGroups];
+  }
   int r0 = 0;
   fetch(0);
   while (r0 < hi) {
@@ -281,9 +285,13 @@ __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void compact_kernel(Com
     for (int i = 0; i < kItems; ++i) {
       const int e = tid + i * B::kThreads, t0 = e % kGroups * 16;
       const uint8_t* row = reinterpret_cast<const uint8_t*>(lds + e / kGroups * B::kRow);
+      // a byte for every token, those of other blocks dropped: the reads wait for nothing
+      uint32_t byte[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) byte[j] = row[(at16[i][j >> 2] >> (8 * (j & 3))) & 0xff];
 #pragma unroll
       for (int j = 0; j < 16; ++j)
-        if (t0 + j >= r0 && t0 + j < r1) w[i][j >> 2] |= (uint32_t)row[map.at[t0 + j]] << (8 * (j & 3));
+        w[i][j >> 2] |= t0 + j >= r0 && t0 + j < r1 ? byte[j] << (8 * (j & 3)) : 0u;
     }
     __syncthreads();
     r0 = r1;
