@@ -381,7 +381,7 @@ trevs_status trevs_rope_frequencies(int32_t rot_dim, double base, int32_t scalin
  * (values are stored with the token last).  A scale is a power of two,
  * 2^-126..2^120: the smallest s with |x| <= 448 s over the block when its rows
  * were written, so that dividing by it is exact and a value is rounded once,
- * to the nearest e4m3 (ties to even).  Rows appended to a block that already
+ * to the nearest e4m3 (ties to even); rows hold magnitudes up to 2^127.  Rows appended to a block that already
  * holds tokens keep its scale or raise it; when it rises, the block's earlier
  * values are rounded again to the new scale (exact above its subnormals).
  *
@@ -501,6 +501,8 @@ typedef struct trevs_kv8_attention_args {
   float* lse;                /* OPTIONAL OUT [B,H_q,T_max] */
 } trevs_kv8_attention_args;
 
+/* About 68 MB at most, and 256 bytes for calls whose tiles of rows fill the GPU by
+ * themselves (0 on invalid args); contents as for the other workspaces. */
 size_t trevs_kv8_attention_workspace_size(const trevs_kv8_cache* cache, const trevs_kv8_attention_args* args);
 trevs_status trevs_kv8_attention(const trevs_kv8_cache* cache, const trevs_kv8_attention_args* args,
                                  void* workspace, size_t workspace_bytes, void* stream);

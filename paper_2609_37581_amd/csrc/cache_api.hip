@@ -179,7 +179,7 @@ trevs_status validate_attention(const trevs_kv8_cache* c, const trevs_kv8_attent
   const int64_t ql = row_ld(a->q_ld, width, e);
   if (!a->q || !a->out || !aligned(a->q, 16) || !aligned(a->out, 16) || !ql) return TREVS_ERR_INVALID_ARG;
   if (!aligned(a->q_len, 4) || !aligned(a->slots, 4) || !aligned(a->lse, 4)) return TREVS_ERR_INVALID_ARG;
-  if (a->H_q > 1024 || rows * a->H_q > INT32_MAX) return TREVS_ERR_UNSUPPORTED;
+  if (a->H_q > 1024 || rows * a->H_q > INT32_MAX - 1024) return TREVS_ERR_UNSUPPORTED;  // (row tiles stay in 32 bits)
   const Rows q{a->q, rows, width * e, ql * e};
   const Span out[] = {{a->out, (size_t)(rows * width * e)}, {a->lse, a->lse ? (size_t)(rows * a->H_q * 4) : 0}};
   const Span in[] = {q.span(), {a->q_len, a->q_len ? (size_t)a->B * 4 : 0}, {a->slots, a->slots ? (size_t)a->B * 4 : 0}};

@@ -130,14 +130,12 @@ __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void write_kernel(Write
   const int start = len - n_new;
   const int j = start / PAGE + f;
   if (n_new == 0 || j * PAGE >= len) return;
-  const int page = page_at(a.c, slot, j);
-  if (page < 0) return;
+  const int page = page_at(a.c, slot, j);  // (on its way while the rows are)
   const int lo = max(start - j * PAGE, 0), hi = min(len - j * PAGE, PAGE);
   const void* src = values ? a.v : a.k;
   const size_t ld = values ? a.v_ld : a.k_ld;
   const size_t row0 = (size_t)b * a.T_max + (j * PAGE - start);  // row of the page's token 0 (may wrap; added to below)
   float x[B::kPer][4][8];
-  float m = 0.f;
 #pragma unroll
   for (int u = 0; u < B::kPer; ++u) {
     const int e = threadIdx.x + u * B::kThreads;
@@ -148,15 +146,21 @@ __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void write_kernel(Write
 #pragma unroll
       for (int q = 0; q < 8; ++q) x[u][i][q] = 0.f;
       if (t >= lo && t < hi) load8(src, (row0 + t) * ld + (size_t)h * D + c, x[u][i], E());
-#pragma unroll
-      for (int q = 0; q < 8; ++q) m = fmaxf(m, fabsf(x[u][i][q]));
     }
   }
+  if (page < 0) return;
   const size_t block = (size_t)page * a.c.H_kv + h;
   float* scale = (values ? a.c.v_scale : a.c.k_scale) + block;
+  const float held = lo > 0 ? *scale : 0.f;
+  float m = 0.f;
+#pragma unroll
+  for (int u = 0; u < B::kPer; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) m = fmaxf(m, fabsf(x[u][i][q]));
   float s = block_scale(block_max<B::kThreads>(m, red)), ratio = 1.f;
   if (lo > 0) {
-    const float held = *scale;
     if (held >= s) {
       s = held;
     } else {
