@@ -12,6 +12,9 @@
  *     token by its max-over-text attention averaged over those heads, take a
  *     stable top-K_2, and compact hidden states, position ids and K/V rows.
  *
+ * The pruned sequence then goes to a serving cache: rotary positions, a paged
+ * K/V cache in 8 bits with the attention that reads it, and its pages.
+ *
  * Conventions for every entry point:
  *   - Tensor pointers are DEVICE pointers to dense row-major tensors.  Float
  *     tensors share one element type per call (trevs_dtype).  Pointers that
