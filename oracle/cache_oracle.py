@@ -183,7 +183,7 @@ class CacheModel:
     def compact(self, kept, src, dst, P, K_in):
         kept = np.asarray(kept)
         for b in range(len(src)):
-            if not self._slot(src[b]) or not self._slot(dst[b]):
+            if not self._slot(src[b]) or not self._slot(dst[b]) or src[b] == dst[b]:
                 continue
             L = self.len[src[b]]
             if L < P + K_in:

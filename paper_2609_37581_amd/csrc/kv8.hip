@@ -208,7 +208,7 @@ __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void compact_kernel(Com
   const int L = slot_len(a.c.len, src, a.c.max_pages * PAGE), room = slot_len(a.c.len, dst, a.c.max_pages * PAGE);
   const int page = dst < 0 ? -1 : page_at(a.c, dst, min(f, a.c.max_pages - 1));
   int from = src < 0 ? -1 : page_at(a.c, src, min(r / PAGE, a.c.max_pages - 1));
-  const int n = L < a.P + a.K_in ? 0 : min(L - a.K_in + a.n_kept, room);
+  const int n = L < a.P + a.K_in || src == dst ? 0 : min(L - a.K_in + a.n_kept, room);
   if (f * PAGE >= n || page < 0) return;
   const int hi = min(n - f * PAGE, PAGE), at = r % PAGE;
   if (tid >= hi) from = -1;

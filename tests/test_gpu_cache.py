@@ -505,6 +505,20 @@ def test_compact(page, H, d):
     check_table(c, m)
 
 
+def test_compact_extremes():
+    """One kept row and all of them, no prefix and nothing after the visual
+    rows; a slot compacted into itself, or into one out of range, is skipped."""
+    rng = np.random.default_rng(21)
+    for K in (1, 70):
+        m = model(rng, [70, 70, 500, 70, K, K, 500], 16, 1, 64)
+        c = device_cache(m)
+        kept = np.sort(np.argsort(rng.random((5, 70)), 1)[:, :K], 1)
+        src, dst = [0, 1, 2, 3, 9], [4, 5, 2, 9, 6]
+        trevs.kv8_compact(c, dev(kept), dev(src), dev(dst), P=0, K_in=70)
+        m.compact(kept, src, dst, 0, 70)
+        check_contents(c, m)
+
+
 # ------------------------------------------------------------------ together
 class Serving:
     """One image with two questions: rotary positions, stage 2, the pruned rows
