@@ -258,7 +258,9 @@ constexpr int kWaves = 4;
 // of value tokens.  Bound by the cache's bytes for single tokens.
 template <class E, int D, int NQ>
 struct RowsShared {
-  float o[16 * NQ][D + 4];
+  // the waves' sums side by side where they fit 34 KB, else added up by one wave after the other
+  static constexpr int kSides = NQ * D <= 128 ? kWaves : 1;
+  float o[kSides][16 * NQ][D + 4];
   float m[kWaves][16 * NQ], l[kWaves][16 * NQ];
 };
 
@@ -436,13 +438,14 @@ __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, R
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) o[i][c] *= f;
   }
-  for (int w = 0; w < kWaves; ++w) {
-    if (wave == w) {
+  constexpr int kSides = RowsShared<E, D, NQ>::kSides;
+  for (int w = 0; w < kWaves; w += kSides) {
+    if (kSides > 1 || wave == w) {
 #pragma unroll
       for (int i = 0; i < NQ; ++i)
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
-          f32x4* at = reinterpret_cast<f32x4*>(&s_o[16 * i + n16][16 * c + 4 * g4]);
+          f32x4* at = reinterpret_cast<f32x4*>(&s_o[kSides > 1 ? wave : 0][16 * i + n16][16 * c + 4 * g4]);
           *at = w == 0 ? o[i][c] : *at + o[i][c];
         }
     }
@@ -457,7 +460,10 @@ __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, R
 #pragma unroll
     for (int w = 0; w < kWaves; ++w)
       if (s_m[w][r] != -INFINITY) sum += s_l[w][r] * exp2f(s_m[w][r] - top);
-    float x[4] = {s_o[r][c], s_o[r][c + 1], s_o[r][c + 2], s_o[r][c + 3]};
+    f32x4 y = *reinterpret_cast<const f32x4*>(&s_o[0][r][c]);
+#pragma unroll
+    for (int w = 1; w < kSides; ++w) y += *reinterpret_cast<const f32x4*>(&s_o[w][r][c]);
+    float x[4] = {y[0], y[1], y[2], y[3]};
     if (pc.part >= 0) {
       const size_t part = (size_t)pc.part * R + r;
       *reinterpret_cast<float4*>(a.part + part * D + c) = make_float4(x[0], x[1], x[2], x[3]);
