@@ -825,14 +825,16 @@ AttnPlan attn_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtype, int
   const long long slots = 256LL * per_cu, side = p.rows == kTileRows ? 1 : kWaves;
   // Uncut, the last round of workgroups leaves `idle` slots without a tile for as long as a tile takes
   // (a step of a workgroup: about 1.5 us, 3 in fp32); cut, a second launch joins the pieces and each piece
-  // begins anew, about 10 us.  Measured, uncut / cut: one token of 64 sequences of 1.2 k to 16.5 k tokens,
-  // 256 tiles for 768 slots, 210 / 115 us; of 32 sequences of 4000 with 16 heads of 64, 512 tiles, 45 / 54;
-  // prompts of 4 x 2048 with 16 heads of 64, 1024 tiles for 512 slots, 65 / 154.  Calls of two rounds or more
-  // are not cut: their long tiles go first, and tiles of a group that run at once share its keys in the L2,
-  // which pieces do not (prompts of 4259 rows, 3728 tiles for 512 slots: 590 / 1085).
-  // The steps of all must fit 31 bits.
-  const long long idle = (tiles + slots - 1) / slots * slots - tiles;
-  const bool cut = tiles < 2 * slots && idle * (steps / side) * (bf16 ? 3 : 6) > 20 * slots && tiles * steps < INT32_MAX;
+  // begins anew, about 10 us, 25 with the staged kernel's larger sums.  Measured, uncut / cut: one token of
+  // 64 sequences of 1.2 k to 16.5 k tokens, 256 tiles for 768 slots, 185 / 107 us; 8 questions over 16.5 k
+  // tokens, 224 for 512, 421 / 220; one token of 32 sequences of 4000 with 16 heads of 64, 512 for 768,
+  // 45 / 54; a prompt of 1024 rows, 224 for 512, 34 / 51; prompts of 4 x 2048 with 16 heads of 64, 1024 for
+  // 512, 65 / 154.  Calls of two rounds or more are not cut: their long tiles go first, and tiles of a group
+  // that run at once share its keys in the L2, which pieces do not (prompts of 4259 rows, 3728 for 512:
+  // 590 / 1085).  The steps of all must fit 31 bits.
+  const long long idle = (tiles + slots - 1) / slots * slots - tiles, begin_us = p.rows == kTileRows ? 25 : 10;
+  const bool cut = tiles < 2 * slots && idle * (steps / side) * (bf16 ? 3 : 6) > 2 * begin_us * slots &&
+                   tiles * steps < INT32_MAX;
   p.pieces = cut ? (int)std::min(slots, (tiles * steps + side - 1) / side) : 0;
   return p;
 }
