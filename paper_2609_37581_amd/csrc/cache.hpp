@@ -163,7 +163,7 @@ struct AttnArgs {
 struct AttnPlan {
   int rows;                 // query rows of a tile
   int row_tiles;
-  int pieces;               // workgroups that the steps of all tiles are cut for, 0: a tile to a workgroup
+  int pieces;               // the most workgroups that the steps of all tiles are cut for, 0: a tile to a workgroup
 };
 AttnPlan attn_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtype, int d_head);
 hipError_t launch_kv8_attention(const AttnArgs& a, const AttnPlan& p, int dtype, int d_head, hipStream_t s);

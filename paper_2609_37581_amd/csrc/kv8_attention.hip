@@ -20,6 +20,7 @@
 // matrix instructions would take keys unconverted, and a bf16 query as two
 // e4m3 parts, but their sums came out 2^-19 off, too far for a log-sum-exp.)
 #include "cache.hpp"
+#include "cut.hpp"
 
 namespace trevs {
 namespace {
@@ -97,11 +98,15 @@ __device__ __forceinline__ void store4(void* out, size_t i, const float (&x)[4],
 constexpr float kSlack = 8.f;
 
 constexpr int kStep = 64;  // tokens of a step
+constexpr int kWaves = 4;
+constexpr int kTileRows = 128;
+// Steps that a workgroup takes side by side: the waves of a staged tile share theirs.
+__host__ __device__ constexpr int side_steps(int rows) { return rows == kTileRows ? 1 : kWaves; }
 
 // A tile is R query rows (t, g) of one group; its steps are the 64-token blocks
 // that its last row sees.  Calls of few tiles, or of uneven ones, cut the
 // steps of all of them, one after the other (sequences, row tiles, groups),
-// into gridDim.x equal pieces, a workgroup to a piece: a piece that covers a
+// into equal pieces, a workgroup to a piece: a piece that covers a
 // tile finishes it, the others leave their sums to join_kernel.  (8 questions
 // over 16.5 k tokens: 225 us; groups before row tiles 238, the same with
 // neighbouring pieces on one XCD.)
@@ -148,14 +153,6 @@ struct Schedule {
     total = __builtin_amdgcn_readlane(ends, 63);
     for (int b0 = 64; b0 < a.B; b0 += 64) total += __builtin_amdgcn_readlane(scan(a, b0), 63);
   }
-  // The first step of workgroup w of n.
-  __device__ __forceinline__ int start(int w, int n) const { return (int)((long long)w * total / n); }
-  // The workgroup that holds a step.
-  __device__ __forceinline__ int owner(int step, int n) const {
-    int w = (int)((long long)step * n / total);
-    while (start(w + 1, n) <= step) ++w;
-    return w;
-  }
 };
 
 // A workgroup's way through its work: in a cut call the pieces of tiles that its steps cover, else one tile.
@@ -168,16 +165,20 @@ struct Piece {
 template <int R>
 struct Walk {
   Schedule<R> s;
+  Cut cut;
   int at, end;         // steps still to do
   Tile t;              // the tile that `at` lies in,
   Sequence seq;        // its sequence,
   int first, n;        // its first step and its steps
-  __device__ __forceinline__ explicit Walk(const AttnArgs& a) : at(0), end(1) {
+  __device__ __forceinline__ explicit Walk(const AttnArgs& a) : cut(0, 0, 1), at(0), end(1) {
     if (!a.part) return;
     s.init(a);
-    at = s.start(blockIdx.x, gridDim.x);
-    end = s.start(blockIdx.x + 1, gridDim.x);
-    if (at < end) locate(a);
+    cut = Cut(s.total, gridDim.x, side_steps(R));
+    end = 0;
+    if ((int)blockIdx.x >= cut.n) return;
+    at = cut.start(blockIdx.x);
+    end = cut.start(blockIdx.x + 1);
+    locate(a);
   }
   __device__ __forceinline__ void locate(const AttnArgs& a) {
     int before = 0, e = s.ends, b0 = 0;
@@ -235,7 +236,7 @@ struct Walk {
     if (p.u0 != 0 || p.u1 != n) p.part = 2 * blockIdx.x + (p.u0 == 0);
     if (p.u0 == 0 && threadIdx.x == 0)
       a.tile_pieces[(t.b * a.c.H_kv + t.hk) * a.row_tiles + t.rt] =
-          make_int2(blockIdx.x, p.part < 0 ? (int)blockIdx.x : s.owner(first + n - 1, gridDim.x));
+          make_int2(blockIdx.x, p.part < 0 ? (int)blockIdx.x : cut.owner(first + n - 1));
     at = first + p.u1;
     if (at < end) advance(a);
     return true;
@@ -250,8 +251,6 @@ __device__ __forceinline__ void store_lse(const AttnArgs& a, const Tile& t, int 
   const int q = r / a.G, h = t.hk * a.G + r - q * a.G;
   a.lse[((size_t)t.b * a.H_q + h) * a.T_max + q] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
-
-constexpr int kWaves = 4;
 
 // A workgroup takes 16 NQ rows of one group; its waves take every kWaves-th
 // step.  Nothing is staged: a lane loads its own 16 bytes of key channels and
@@ -497,7 +496,6 @@ __global__ __launch_bounds__(kWaves * 64, NQ == 1 && D <= 128 && E::kBytes == 2 
 // The clock under load bounds both (518 us with all-zero data): logits formed
 // half a step ahead of the exponentials, operands staged as bf16 (a third fewer
 // vector instructions) and 256 rows a workgroup each took the same within 3 %.
-constexpr int kTileRows = 128;
 
 // Permutation of a staged row's 16-byte columns, by the row: 16 lanes next to
 // each other read one column of 16 rows and must meet 16 different ones modulo
@@ -822,7 +820,7 @@ AttnPlan attn_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtype, int
   const long long tiles = (long long)B * H_kv * p.row_tiles, steps = (kv_max + kStep - 1) / kStep;
   // workgroups that run at once, and the steps that one takes side by side
   const int per_cu = d_head == 256 || p.rows == 32 ? 1 : p.rows == 16 && bf16 ? 3 : 2;
-  const long long slots = 256LL * per_cu, side = p.rows == kTileRows ? 1 : kWaves;
+  const long long slots = 256LL * per_cu, side = side_steps(p.rows);
   // Uncut, the last round of workgroups leaves `idle` slots without a tile for as long as a tile takes
   // (a step of a workgroup: about 1.5 us, 3 in fp32); cut, a second launch joins the pieces and each piece
   // begins anew, about 10 us, 25 with the staged kernel's larger sums.  Measured, uncut / cut: one token of
