@@ -325,7 +325,9 @@ __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void compact_kernel(Com
       float x[4];
       from_e4m3(w[i][j], x);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) x[q] *= map.scale[t0 + 4 * j + q] * inv;
+      // (one factor after the other: a block of zeros has the smallest scale, and the product of the two
+      // passes fp32's range)
+      for (int q = 0; q < 4; ++q) x[q] = x[q] * map.scale[t0 + 4 * j + q] * inv;
       const int n_t = hi - t0 - 4 * j;  // tokens of this word
       const uint32_t mask = n_t >= 4 ? ~0u : n_t <= 0 ? 0u : (1u << (8 * n_t)) - 1u;
       y[j] = (to_e4m3(x[0], x[1], x[2], x[3]) & mask) | (y[j] & ~mask);

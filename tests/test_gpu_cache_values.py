@@ -1,0 +1,37 @@
+"""Values at the ends of the 8-bit cache's range."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_37581_amd import trevs
+from test_gpu_cache import check_contents, dev, device_cache, model, storage
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("page,d", [(16, 64), (32, 256), (64, 128)])
+@pytest.mark.parametrize("top", [2000.0, 2.0 ** 100, 2.0 ** 127])
+def test_compact_zero_rows_of_large_blocks(page, d, top):
+    """Kept rows that are zero, or far below their page's largest value, which is
+    dropped: a destination of zeros has the smallest scale, far from its source's."""
+    rng = np.random.default_rng(page)
+    P, K_in, K, T = 3, 5 * page, 2 * page, 7
+    S = P + K_in + T
+    m = model(rng, [S] * 2 + [P + K + T] * 2, page, 2, d, n_layers=2)
+    x = np.zeros((2, S, 2, d))
+    x[:, P + 1:P + K_in:2] = top * rng.normal(size=x[:, P + 1:P + K_in:2].shape).clip(-1, 1)  # rows that are dropped
+    x[1, P:P + K_in:4, :, 5] = top * 2.0 ** -17  # (of e4m3 the smallest number or zero)
+    x[1, P + 2:P + K_in:4] = 2.0 ** -120
+    k, xs = storage(x, torch.float32)
+    c = device_cache(m)
+    for layer in (0, 1):
+        trevs.kv8_write(c, k, -k, slots=dev([0, 1]), layer=layer)
+        m.write(xs, -xs, slots=[0, 1], layer=layer)
+    kept = np.broadcast_to(np.arange(0, K_in, 2)[:K], (2, K)).copy()
+    trevs.kv8_compact(c, dev(kept), dev([0, 1]), dev([2, 3]), P=P, K_in=K_in)
+    m.compact(kept, [0, 1], [2, 3], P, K_in)
+    check_contents(c, m)
+    q, qs = storage(rng.normal(size=(2, 1, 4, d)) * 2.0 ** -120, torch.float32)
+    out = trevs.kv8_attention(c, q, slots=dev([2, 3]))
+    torch.cuda.synchronize()
+    assert torch.isfinite(out).all()
