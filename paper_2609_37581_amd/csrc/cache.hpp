@@ -128,7 +128,8 @@ struct CompactArgs {
   const int32_t* src;
   const int32_t* dst;
   int B, P, K_in, n_kept, n_layers;
-  int frames;               // pages of the longest sequence
+  int frames;               // blocks of a sequence and head that the launch has workgroups for;
+  int turns;                // others are taken in turns (0: there are none)
 };
 hipError_t launch_kv8_compact(const CompactArgs& a, int d_head, int page, hipStream_t s);
 

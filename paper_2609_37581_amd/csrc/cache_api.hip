@@ -216,12 +216,23 @@ trevs_status validate_compact(const trevs_kv8_cache* c, const trevs_kv8_compact_
   if (!aligned(a->kept_idx, 4) || !aligned(a->src_slots, 4) || !aligned(a->dst_slots, 4)) return TREVS_ERR_INVALID_ARG;
   if ((int64_t)a->P + a->K_in > (int64_t)c->max_pages * c->page_tokens) return TREVS_ERR_INVALID_ARG;
   if ((int64_t)a->B * a->n_kept > INT32_MAX) return TREVS_ERR_UNSUPPORTED;
-  if ((int64_t)c->n_layers * a->B * c->max_pages > INT32_MAX / c->H_kv) return TREVS_ERR_UNSUPPORTED;
+  if ((int64_t)c->n_layers * a->B * c->H_kv > kMaxGroups) return TREVS_ERR_UNSUPPORTED;
   const size_t B = a->B;
   if (meets_cache(c, Span{a->kept_idx, B * a->n_kept * 4}) || meets_cache(c, Span{a->src_slots, B * 4}) ||
       meets_cache(c, Span{a->dst_slots, B * 4}))
     return TREVS_ERR_INVALID_ARG;
   return TREVS_OK;
+}
+
+// The compaction's launch: the sequences' lengths are on the device, so it has a workgroup for every block that
+// the table can hold (a shorter source is skipped), unless that is more than twice what the prefix and the kept
+// rows fill twice, or 8192 workgroups of keys and values: longer sequences' blocks are then taken in turns.
+void plan_compact(const trevs_kv8_cache* c, const trevs_kv8_compact_args* a, CompactArgs* t) {
+  const int64_t each = (int64_t)c->n_layers * a->B * c->H_kv, page = c->page_tokens;
+  const int64_t table = ((int64_t)c->max_pages * page - a->K_in + a->n_kept + page - 1) / page;
+  const int64_t wanted = std::max(2 * (((int64_t)a->P + a->n_kept + page - 1) / page), 4096 / each);
+  t->frames = (int)std::min(table > 2 * wanted ? wanted : table, kMaxGroups / each);
+  t->turns = t->frames < table;
 }
 
 }  // namespace
@@ -412,8 +423,7 @@ trevs_status trevs_kv8_compact(const trevs_kv8_cache* c, const trevs_kv8_compact
   t.K_in = a->K_in;
   t.n_kept = a->n_kept;
   t.n_layers = c->n_layers;
-  // (a shorter source is skipped, a longer one there is none)
-  t.frames = (int)(((int64_t)c->max_pages * c->page_tokens - a->K_in + a->n_kept + c->page_tokens - 1) / c->page_tokens);
+  plan_compact(c, a, &t);
   TREVS_HIP(launch_kv8_compact(t, c->d_head, c->page_tokens, reinterpret_cast<hipStream_t>(stream)));
   return TREVS_OK;
 }

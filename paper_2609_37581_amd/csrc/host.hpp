@@ -39,6 +39,9 @@ inline bool any_overlap(const Span* out, int n_out, const Span* in, int n_in) {
   return false;
 }
 
+// Workgroups in x of a launch with blocks of up to 256 threads: its threads are counted in 32 bits.
+constexpr int64_t kMaxGroups = UINT32_MAX / 256;
+
 inline trevs_status check_ws(void* ws, size_t ws_bytes, size_t need) {
   if (need == 0) return TREVS_OK;
   if (!ws || ws_bytes < need || !aligned(ws, kWsAlign)) return TREVS_ERR_WORKSPACE;

@@ -184,7 +184,12 @@ struct TokenMap {
 // source block that its tokens name into LDS whole, 16 bytes a lane, and takes
 // the bytes from there (single bytes from memory, a line each: 37.5 us for 4
 // layers of 4 x 1187 of 4259 tokens, this way 20).
-template <int D, int PAGE>
+//
+// With TURNS a workgroup goes on to every frames-th block after its first; without, the launch has one for every
+// block that the table can hold.  (4 and 28 layers of 4 sequences, 1187 of 4259 tokens of 4 heads of 128, the table
+// 4 and 20 times as long as they are: without 48, 206 and 291, 1432 us, with 32, 32 and 151, 147; as long as they
+// are, without: 20 and 109.)
+template <int D, int PAGE, bool TURNS>
 __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void compact_kernel(CompactArgs a) {
   using B = Block<D, PAGE>;
   __shared__ uint32_t lds[D * B::kRow];
@@ -193,148 +198,157 @@ __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void compact_kernel(Com
   __shared__ uint64_t s_runs;
   const bool values = blockIdx.y != 0;
   const int tid = threadIdx.x;
-  long long id = blockIdx.x;
+  unsigned id = blockIdx.x;
   const int h = (int)(id % a.c.H_kv);
   id /= a.c.H_kv;
-  const int f = (int)(id % a.frames);
+  int f = (int)(id % a.frames);
   id /= a.frames;
   const int b = (int)(id % a.B), layer = (int)(id / a.B);
   // the loads that depend on each other go out in three steps: slots and kept rows, lengths and pages,
   // scales and data (the bounds are checked on what came back)
   const int src = slot_of(a.src, b, a.c.n_slots), dst = slot_of(a.dst, b, a.c.n_slots);
-  int r = f * PAGE + min(tid, PAGE - 1);
-  const int kept = a.kept[(size_t)b * a.n_kept + min(max(r - a.P, 0), a.n_kept - 1)];
-  r = r >= a.P + a.n_kept ? r + a.K_in - a.n_kept : r >= a.P ? a.P + min(max(kept, 0), a.K_in - 1) : r;
-  const int L = slot_len(a.c.len, src, a.c.max_pages * PAGE), room = slot_len(a.c.len, dst, a.c.max_pages * PAGE);
-  const int page = dst < 0 ? -1 : page_at(a.c, dst, min(f, a.c.max_pages - 1));
-  int from = src < 0 ? -1 : page_at(a.c, src, min(r / PAGE, a.c.max_pages - 1));
-  const int n = L < a.P + a.K_in || src == dst ? 0 : min(L - a.K_in + a.n_kept, room);
-  if (f * PAGE >= n || page < 0) return;
-  const int hi = min(n - f * PAGE, PAGE), at = r % PAGE;
-  if (tid >= hi) from = -1;
-  const size_t layer_blocks = (size_t)layer * a.c.n_pages * a.c.H_kv;
-  const uint8_t* data = (values ? a.c.v : a.c.k) + (layer_blocks + h) * (PAGE * D);
-  const float* scales = (values ? a.c.v_scale : a.c.k_scale) + layer_blocks + h;
-  if (tid < 64) {
-    if (tid < PAGE) {
-      map.block[tid] = from;
-      reinterpret_cast<uint8_t*>(map.at)[tid] = (uint8_t)at;
-      map.scale[tid] = from >= 0 ? scales[(size_t)from * a.c.H_kv] : 0.f;
-    }
-    const int before = __shfl_up(from, 1, 64);
-    const uint64_t starts = __ballot(tid < hi && (tid == 0 || from != before));
-    if (tid == 0) s_runs = starts;  // tokens whose page is not the one before's
-  }
-  __syncthreads();
-  const size_t block = layer_blocks + (size_t)page * a.c.H_kv + h;
-  if (!values) {
-    float x[B::kPer][4][8], m = 0.f;
-#pragma unroll
-    for (int u = 0; u < B::kPer; ++u) {
-      const int e = tid + u * B::kThreads;
-      const int c = e % (D / 8) * 8, t0 = e / (D / 8) * 4;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = t0 + i;
-        const int from = t < hi ? map.block[t] : -1;
-        const u32x2 w = from >= 0 ? *reinterpret_cast<const u32x2*>(data + (size_t)from * a.c.H_kv * (PAGE * D) +
-                                                                    reinterpret_cast<const uint8_t*>(map.at)[t] * D + c)
-                                  : u32x2{0u, 0u};
-        float y[2][4];
-        from_e4m3(w[0], y[0]);
-        from_e4m3(w[1], y[1]);
-        const float s = from >= 0 ? map.scale[t] : 0.f;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          x[u][i][q] = y[q >> 2][q & 3] * s;
-          m = fmaxf(m, fabsf(x[u][i][q]));
+  while (true) {
+    int r = f * PAGE + min(tid, PAGE - 1);
+    const int kept = a.kept[(size_t)b * a.n_kept + min(max(r - a.P, 0), a.n_kept - 1)];
+    r = r >= a.P + a.n_kept ? r + a.K_in - a.n_kept : r >= a.P ? a.P + min(max(kept, 0), a.K_in - 1) : r;
+    const int L = slot_len(a.c.len, src, a.c.max_pages * PAGE), room = slot_len(a.c.len, dst, a.c.max_pages * PAGE);
+    const int page = dst < 0 ? -1 : page_at(a.c, dst, min(f, a.c.max_pages - 1));
+    int from = src < 0 ? -1 : page_at(a.c, src, min(r / PAGE, a.c.max_pages - 1));
+    const int n = L < a.P + a.K_in || src == dst ? 0 : min(L - a.K_in + a.n_kept, room);
+    if (f * PAGE >= n) return;
+    if (page >= 0) {
+      const int hi = min(n - f * PAGE, PAGE), at = r % PAGE;
+      if (tid >= hi) from = -1;
+      const size_t layer_blocks = (size_t)layer * a.c.n_pages * a.c.H_kv;
+      const uint8_t* data = (values ? a.c.v : a.c.k) + (layer_blocks + h) * (PAGE * D);
+      const float* scales = (values ? a.c.v_scale : a.c.k_scale) + layer_blocks + h;
+      if (tid < 64) {
+        if (tid < PAGE) {
+          map.block[tid] = from;
+          reinterpret_cast<uint8_t*>(map.at)[tid] = (uint8_t)at;
+          map.scale[tid] = from >= 0 ? scales[(size_t)from * a.c.H_kv] : 0.f;
         }
+        const int before = __shfl_up(from, 1, 64);
+        const uint64_t starts = __ballot(tid < hi && (tid == 0 || from != before));
+        if (tid == 0) s_runs = starts;  // tokens whose page is not the one before's
+      }
+      __syncthreads();
+      const size_t block = layer_blocks + (size_t)page * a.c.H_kv + h;
+      if (!values) {
+        float x[B::kPer][4][8], m = 0.f;
+#pragma unroll
+        for (int u = 0; u < B::kPer; ++u) {
+          const int e = tid + u * B::kThreads;
+          const int c = e % (D / 8) * 8, t0 = e / (D / 8) * 4;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int t = t0 + i;
+            const int from = t < hi ? map.block[t] : -1;
+            const int row = reinterpret_cast<const uint8_t*>(map.at)[t];
+            const u32x2 w = from >= 0 ? *reinterpret_cast<const u32x2*>(data + (size_t)from * a.c.H_kv * (PAGE * D) +
+                                                                        row * D + c)
+                                      : u32x2{0u, 0u};
+            float y[2][4];
+            from_e4m3(w[0], y[0]);
+            from_e4m3(w[1], y[1]);
+            const float s = from >= 0 ? map.scale[t] : 0.f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              x[u][i][q] = y[q >> 2][q & 3] * s;
+              m = fmaxf(m, fabsf(x[u][i][q]));
+            }
+          }
+        }
+        const float s = block_scale(block_max<B::kThreads>(m, red));
+        store_block<D, PAGE>(a.c.k + block * (PAGE * D), false, 0, hi, pow2_inverse(s), 1.f, x, lds);
+        if (tid == 0) a.c.k_scale[block] = s;
+      } else {
+        // a thread's items: 16 tokens of a channel, as bytes
+        constexpr int kGroups = PAGE / 16, kItems = D * kGroups / B::kThreads;
+        static_assert(kItems * B::kThreads == D * kGroups, "whole items");
+        u32x4 w[kItems], next[kItems], at16[kItems];
+        uint64_t runs = s_runs;
+        auto fetch = [&](int t) {
+          const int from = map.block[t];
+#pragma unroll
+          for (int i = 0; i < kItems; ++i)
+            next[i] = from >= 0 ? ldg16(data + (size_t)from * a.c.H_kv * (PAGE * D) + (tid + i * B::kThreads) * 16)
+                                : zero4();
+        };
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+          w[i] = zero4();
+          at16[i] = map.at[(tid + i * B::kThreads) % kGroups];
+        }
+        int r0 = 0;
+        fetch(0);
+        while (r0 < hi) {
+          runs &= runs - 1;
+          const int r1 = runs ? __builtin_ctzll(runs) : hi;
+#pragma unroll
+          for (int i = 0; i < kItems; ++i) {
+            const int e = tid + i * B::kThreads;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) lds[e / kGroups * B::kRow + e % kGroups * 4 + j] = next[i][j];
+          }
+          __syncthreads();
+          if (r1 < hi) fetch(r1);
+#pragma unroll
+          for (int i = 0; i < kItems; ++i) {
+            const int e = tid + i * B::kThreads, t0 = e % kGroups * 16;
+            const uint8_t* row = reinterpret_cast<const uint8_t*>(lds + e / kGroups * B::kRow);
+            // a byte for every token, those of other blocks dropped: the reads wait for nothing
+            uint32_t byte[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) byte[j] = row[(at16[i][j >> 2] >> (8 * (j & 3))) & 0xff];
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              w[i][j >> 2] |= t0 + j >= r0 && t0 + j < r1 ? byte[j] << (8 * (j & 3)) : 0u;
+          }
+          __syncthreads();
+          r0 = r1;
+        }
+        float m = 0.f;
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+          const int t0 = (tid + i * B::kThreads) % kGroups * 16;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float y[4];
+            from_e4m3(w[i][j], y);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) m = fmaxf(m, fabsf(y[q]) * map.scale[t0 + 4 * j + q]);
+          }
+        }
+        const float s = block_scale(block_max<B::kThreads>(m, red)), inv = pow2_inverse(s);
+        uint8_t* out = a.c.v + block * (PAGE * D);
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+          const int e = tid + i * B::kThreads, t0 = e % kGroups * 16;
+          if (t0 >= hi) continue;
+          u32x4* to = reinterpret_cast<u32x4*>(out + e * 16);
+          u32x4 y = t0 + 16 > hi ? *to : zero4();  // tokens past the last are kept
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float x[4];
+            from_e4m3(w[i][j], x);
+#pragma unroll
+            // (one factor after the other: a block of zeros has the smallest scale, and the product of the two
+            // passes fp32's range)
+            for (int q = 0; q < 4; ++q) x[q] = x[q] * map.scale[t0 + 4 * j + q] * inv;
+            const int n_t = hi - t0 - 4 * j;  // tokens of this word
+            const uint32_t mask = n_t >= 4 ? ~0u : n_t <= 0 ? 0u : (1u << (8 * n_t)) - 1u;
+            y[j] = (to_e4m3(x[0], x[1], x[2], x[3]) & mask) | (y[j] & ~mask);
+          }
+          *to = y;
+        }
+        if (tid == 0) a.c.v_scale[block] = s;
       }
     }
-    const float s = block_scale(block_max<B::kThreads>(m, red));
-    store_block<D, PAGE>(a.c.k + block * (PAGE * D), false, 0, hi, pow2_inverse(s), 1.f, x, lds);
-    if (tid == 0) a.c.k_scale[block] = s;
-    return;
+    if (!TURNS || f + a.frames > (n - 1) / PAGE) return;
+    f += a.frames;
+    __syncthreads();  // the block's LDS is read before the next one's is written
   }
-  // a thread's items: 16 tokens of a channel, as bytes
-  constexpr int kGroups = PAGE / 16, kItems = D * kGroups / B::kThreads;
-  static_assert(kItems * B::kThreads == D * kGroups, "whole items");
-  u32x4 w[kItems], next[kItems], at16[kItems];
-  uint64_t runs = s_runs;
-  auto fetch = [&](int t) {
-    const int from = map.block[t];
-#pragma unroll
-    for (int i = 0; i < kItems; ++i)
-      next[i] = from >= 0 ? ldg16(data + (size_t)from * a.c.H_kv * (PAGE * D) + (tid + i * B::kThreads) * 16) : zero4();
-  };
-#pragma unroll
-  for (int i = 0; i < kItems; ++i) {
-    w[i] = zero4();
-    at16[i] = map.at[(tid + i * B::kThreads) % kGroups];
-  }
-  int r0 = 0;
-  fetch(0);
-  while (r0 < hi) {
-    runs &= runs - 1;
-    const int r1 = runs ? __builtin_ctzll(runs) : hi;
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      const int e = tid + i * B::kThreads;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) lds[e / kGroups * B::kRow + e % kGroups * 4 + j] = next[i][j];
-    }
-    __syncthreads();
-    if (r1 < hi) fetch(r1);
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      const int e = tid + i * B::kThreads, t0 = e % kGroups * 16;
-      const uint8_t* row = reinterpret_cast<const uint8_t*>(lds + e / kGroups * B::kRow);
-      // a byte for every token, those of other blocks dropped: the reads wait for nothing
-      uint32_t byte[16];
-#pragma unroll
-      for (int j = 0; j < 16; ++j) byte[j] = row[(at16[i][j >> 2] >> (8 * (j & 3))) & 0xff];
-#pragma unroll
-      for (int j = 0; j < 16; ++j)
-        w[i][j >> 2] |= t0 + j >= r0 && t0 + j < r1 ? byte[j] << (8 * (j & 3)) : 0u;
-    }
-    __syncthreads();
-    r0 = r1;
-  }
-  float m = 0.f;
-#pragma unroll
-  for (int i = 0; i < kItems; ++i) {
-    const int t0 = (tid + i * B::kThreads) % kGroups * 16;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float y[4];
-      from_e4m3(w[i][j], y);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) m = fmaxf(m, fabsf(y[q]) * map.scale[t0 + 4 * j + q]);
-    }
-  }
-  const float s = block_scale(block_max<B::kThreads>(m, red)), inv = pow2_inverse(s);
-  uint8_t* out = a.c.v + block * (PAGE * D);
-#pragma unroll
-  for (int i = 0; i < kItems; ++i) {
-    const int e = tid + i * B::kThreads, t0 = e % kGroups * 16;
-    if (t0 >= hi) continue;
-    u32x4* to = reinterpret_cast<u32x4*>(out + e * 16);
-    u32x4 y = t0 + 16 > hi ? *to : zero4();  // tokens past the last are kept
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float x[4];
-      from_e4m3(w[i][j], x);
-#pragma unroll
-      // (one factor after the other: a block of zeros has the smallest scale, and the product of the two
-      // passes fp32's range)
-      for (int q = 0; q < 4; ++q) x[q] = x[q] * map.scale[t0 + 4 * j + q] * inv;
-      const int n_t = hi - t0 - 4 * j;  // tokens of this word
-      const uint32_t mask = n_t >= 4 ? ~0u : n_t <= 0 ? 0u : (1u << (8 * n_t)) - 1u;
-      y[j] = (to_e4m3(x[0], x[1], x[2], x[3]) & mask) | (y[j] & ~mask);
-    }
-    *to = y;
-  }
-  if (tid == 0) a.c.v_scale[block] = s;
 }
 
 // Pair i's page in layer z, 16 bytes a lane and step.
@@ -384,10 +398,14 @@ hipError_t launch_kv8_write(const WriteArgs& a, int dtype, int d_head, int page,
 }
 
 hipError_t launch_kv8_compact(const CompactArgs& a, int d_head, int page, hipStream_t s) {
-  const dim3 grid((unsigned)((long long)a.n_layers * a.B * a.frames * a.c.H_kv), 2);
+  const dim3 grid((unsigned)a.n_layers * a.B * a.frames * a.c.H_kv, 2);
   return by_shape(d_head, page, [&](auto d, auto p) {
     constexpr int D = decltype(d)::value, PAGE = decltype(p)::value;
-    hipLaunchKernelGGL((compact_kernel<D, PAGE>), grid, dim3(Block<D, PAGE>::kThreads), 0, s, a);
+    const dim3 block(Block<D, PAGE>::kThreads);
+    if (a.turns)
+      hipLaunchKernelGGL((compact_kernel<D, PAGE, true>), grid, block, 0, s, a);
+    else
+      hipLaunchKernelGGL((compact_kernel<D, PAGE, false>), grid, block, 0, s, a);
   });
 }
 
