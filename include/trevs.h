@@ -452,8 +452,8 @@ trevs_status trevs_pages_free(const trevs_kv8_cache* cache, int32_t n, const int
 
 /* Pages src[i] copied to pages dst[i] in every layer, keys, values and scales
  * (bit copies); pairs with an entry out of range are skipped.  No page may be
- * the destination of two pairs, nor of one and the source of another.  n is
- * not limited here. */
+ * the destination of two pairs, nor of one and the source of another.  n is at
+ * most 2^24 - 1. */
 trevs_status trevs_kv8_copy_pages(const trevs_kv8_cache* cache, int32_t n, const int32_t* src,
                                   const int32_t* dst, void* stream);
 

@@ -109,6 +109,7 @@ struct RopeArgs {
   float attn_factor;        // negated sine for the inverse is `sign`
   float sign;
 };
+int rope_rows(long long rows, int rot_dim);  // rows of a workgroup
 hipError_t launch_rope(const RopeArgs& a, int interleaved, int dtype, hipStream_t s);
 
 struct WriteArgs {

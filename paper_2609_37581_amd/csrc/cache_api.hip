@@ -63,6 +63,8 @@ trevs_status validate_rope(const trevs_rope_args* a) {
   if (!head_size_ok(a->d_head)) return TREVS_ERR_UNSUPPORTED;
   const int64_t rows = (int64_t)a->B * a->S;
   if (rows * a->n_pos > INT32_MAX || a->H_q > 1024 || a->H_k > 1024) return TREVS_ERR_UNSUPPORTED;
+  const int per_group = rope_rows(rows, a->rot_dim);
+  if ((rows + per_group - 1) / per_group > kMaxGroups) return TREVS_ERR_UNSUPPORTED;
   Rows src[2] = {}, dst[2] = {};
   for (int i = 0; i < 2; ++i) {
     if (H[i] == 0) continue;
@@ -157,12 +159,19 @@ trevs_status validate_write(const trevs_kv8_cache* c, const trevs_kv8_write_args
   if (!aligned(a->n_new, 4) || !aligned(a->slots, 4)) return TREVS_ERR_INVALID_ARG;
   if (rows > INT32_MAX) return TREVS_ERR_UNSUPPORTED;
   const int64_t frames = ((int64_t)a->T_max + c->page_tokens - 2) / c->page_tokens + 1;
-  if (a->B * frames * c->H_kv > INT32_MAX) return TREVS_ERR_UNSUPPORTED;
+  if (a->B * frames * c->H_kv > kMaxGroups) return TREVS_ERR_UNSUPPORTED;
   const Rows k{a->k, rows, width * e, kl * e}, v{a->v, rows, width * e, vl * e};
   if (meets_cache(c, k.span()) || meets_cache(c, v.span()) || meets_cache(c, Span{a->n_new, (size_t)a->B * 4}) ||
       meets_cache(c, Span{a->slots, (size_t)a->B * 4}))
     return TREVS_ERR_INVALID_ARG;
   return TREVS_OK;
+}
+
+int max_keys(const trevs_kv8_cache* c, const trevs_kv8_attention_args* a) {
+  return a->kv_max ? a->kv_max : c->max_pages * c->page_tokens;
+}
+AttnPlan plan_of(const trevs_kv8_cache* c, const trevs_kv8_attention_args* a) {
+  return attn_plan(a->B, a->T_max, c->H_kv, a->H_q / c->H_kv, max_keys(c, a), a->dtype, c->d_head);
 }
 
 trevs_status validate_attention(const trevs_kv8_cache* c, const trevs_kv8_attention_args* a) {
@@ -186,11 +195,8 @@ trevs_status validate_attention(const trevs_kv8_cache* c, const trevs_kv8_attent
   if (any_overlap(out, 2, in, 3)) return TREVS_ERR_INVALID_ARG;
   for (const Span& o : out)
     if (meets_cache(c, o)) return TREVS_ERR_INVALID_ARG;
+  if ((int64_t)a->B * c->H_kv * plan_of(c, a).row_tiles > kMaxGroups) return TREVS_ERR_UNSUPPORTED;
   return TREVS_OK;
-}
-
-int max_keys(const trevs_kv8_cache* c, const trevs_kv8_attention_args* a) {
-  return a->kv_max ? a->kv_max : c->max_pages * c->page_tokens;
 }
 
 // Cut calls: the tiles' pieces, then their sums: (maximum, sum) pairs and values.
@@ -200,7 +206,7 @@ struct AttnLayout {
 };
 AttnLayout attention_layout(const trevs_kv8_cache* c, const trevs_kv8_attention_args* a) {
   AttnLayout L;
-  L.plan = attn_plan(a->B, a->T_max, c->H_kv, a->H_q / c->H_kv, max_keys(c, a), a->dtype, c->d_head);
+  L.plan = plan_of(c, a);
   const size_t parts = (size_t)2 * L.plan.pieces * L.plan.rows;
   L.part_ml = parts ? align_up((size_t)a->B * c->H_kv * L.plan.row_tiles * sizeof(int2)) : 0;
   L.part = L.part_ml + align_up(parts * sizeof(float2));
@@ -342,6 +348,7 @@ trevs_status trevs_kv8_copy_pages(const trevs_kv8_cache* c, int32_t n, const int
                                   void* stream) {
   TREVS_TRY(validate_cache(c));
   if (n < 1 || !src || !dst || !aligned(src, 4) || !aligned(dst, 4)) return TREVS_ERR_INVALID_ARG;
+  if (n > kMaxGroups) return TREVS_ERR_UNSUPPORTED;
   if (meets_cache(c, Span{src, (size_t)n * 4}) || meets_cache(c, Span{dst, (size_t)n * 4}))
     return TREVS_ERR_INVALID_ARG;
   CopyArgs a;

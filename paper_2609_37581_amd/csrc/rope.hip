@@ -119,11 +119,16 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int rows_per
 
 }  // namespace
 
+int rope_rows(long long rows, int rot_dim) {
+  // one sine and cosine a thread; fewer rows when the rows would not give every CU a workgroup
+  int n = min(kMaxRows, max(1, 2 * kThreads / rot_dim));
+  while (n > 1 && (rows + n - 1) / n < 512) n >>= 1;
+  return n;
+}
+
 hipError_t launch_rope(const RopeArgs& a, int interleaved, int dtype, hipStream_t s) {
   const int half = a.rot_dim / 2;
-  // one sine and cosine a thread; fewer rows when the rows would not give every CU a workgroup
-  int rows = min(kMaxRows, max(1, kThreads / half));
-  while (rows > 1 && (a.rows + rows - 1) / rows < 512) rows >>= 1;
+  const int rows = rope_rows(a.rows, a.rot_dim);
   const long long blocks = (a.rows + rows - 1) / rows;
   // a few rows split their heads over workgroups
   const int ve = 16 / (dtype == TREVS_BF16 ? 2 : 4);
