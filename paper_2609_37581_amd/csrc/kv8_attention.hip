@@ -249,7 +249,8 @@ __device__ __forceinline__ size_t out_row(const AttnArgs& a, const Tile& t, int 
 }
 __device__ __forceinline__ void store_lse(const AttnArgs& a, const Tile& t, int r, float m, float l) {
   const int q = r / a.G, h = t.hk * a.G + r - q * a.G;
-  a.lse[((size_t)t.b * a.H_q + h) * a.T_max + q] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+  // (l is 0 for a row that sees no key, and NaN, as its outputs, for one that sees a NaN)
+  a.lse[((size_t)t.b * a.H_q + h) * a.T_max + q] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 // A workgroup takes 16 NQ rows of one group; its waves take every kWaves-th
@@ -457,8 +458,8 @@ __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, R
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-      if (s_m[w][r] != -INFINITY) sum += s_l[w][r] * exp2f(s_m[w][r] - top);
+    for (int w = 0; w < kWaves; ++w)  // (a NaN logit leaves the maximum at -inf and makes the sum NaN)
+      sum += s_l[w][r] * (s_m[w][r] == -INFINITY ? 0.f : exp2f(s_m[w][r] - top));
     f32x4 y = *reinterpret_cast<const f32x4*>(&s_o[0][r][c]);
 #pragma unroll
     for (int w = 1; w < kSides; ++w) y += *reinterpret_cast<const f32x4*>(&s_o[w][r][c]);
