@@ -384,9 +384,12 @@ trevs_status trevs_rope_frequencies(int32_t rot_dim, double base, int32_t scalin
  * (values are stored with the token last).  A scale is a power of two,
  * 2^-126..2^120: the smallest s with |x| <= 448 s over the block when its rows
  * were written, so that dividing by it is exact and a value is rounded once,
- * to the nearest e4m3 (ties to even); rows hold magnitudes up to 2^127.  Rows appended to a block that already
- * holds tokens keep its scale or raise it; when it rises, the block's earlier
- * values are rounded again to the new scale (exact above its subnormals).
+ * to the nearest e4m3 (ties to even); rows hold magnitudes up to 2^127.  Rows
+ * should be finite: an infinity or NaN is stored as NaN and does not count for
+ * the scale, so the block's other values are as without it.  Rows appended to
+ * a block that already holds tokens keep its scale or raise it; when it rises,
+ * the block's earlier values are rounded again to the new scale (exact above
+ * its subnormals).
  *
  * One page table serves every layer: sequence slot i < n_slots holds len[i]
  * tokens, token t in page table[i][t / page_tokens].  ref[p] counts the slots

@@ -6,6 +6,8 @@
 // conversion.  Lanes hold units of 4 tokens x 8 channels: keys are stored 8
 // channels at a time, values (token last) are turned in LDS, four tokens to a
 // word.
+#include <float.h>
+
 #include "cache.hpp"
 
 namespace trevs {
@@ -152,14 +154,24 @@ __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void write_kernel(Write
   const size_t block = (size_t)page * a.c.H_kv + h;
   float* scale = (values ? a.c.v_scale : a.c.k_scale) + block;
   const float held = lo > 0 ? *scale : 0.f;
-  float m = 0.f;
+  // The block's largest magnitude: fmaxf passes NaN by, and infinities, if it finds one, are left out in a second
+  // try.  (Both are stored as NaN by the conversion, the other values with the scale that these need.)
+  auto largest = [&](float below) {
+    float m = 0.f;
 #pragma unroll
-  for (int u = 0; u < B::kPer; ++u)
+    for (int u = 0; u < B::kPer; ++u)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int q = 0; q < 8; ++q) m = fmaxf(m, fabsf(x[u][i][q]));
-  float s = block_scale(block_max<B::kThreads>(m, red)), ratio = 1.f;
+        for (int q = 0; q < 8; ++q) m = fabsf(x[u][i][q]) > below ? m : fmaxf(m, fabsf(x[u][i][q]));
+    return block_max<B::kThreads>(m, red);
+  };
+  float m = largest(INFINITY);
+  if (m == INFINITY) {
+    __syncthreads();  // (every thread has the same m)
+    m = largest(FLT_MAX);
+  }
+  float s = block_scale(m), ratio = 1.f;
   if (lo > 0) {
     if (held >= s) {
       s = held;

@@ -1,10 +1,12 @@
 """Values at the ends of the 8-bit cache's range."""
+import math
+
 import numpy as np
 import pytest
 import torch
 
 from paper_2609_37581_amd import trevs
-from test_gpu_cache import check_attention, check_contents, dev, device_cache, model, storage
+from test_gpu_cache import TABLE, check_attention, check_contents, dev, device_cache, model, storage
 
 pytestmark = pytest.mark.gpu
 
@@ -35,6 +37,36 @@ def test_compact_zero_rows_of_large_blocks(page, d, top):
     out = trevs.kv8_attention(c, q, slots=dev([2, 3]))
     torch.cuda.synchronize()
     assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("page,d", [(16, 128), (64, 64)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_write_infinities_and_nan(page, d, dtype):
+    """Numbers that are not finite are stored as NaN, and the rest of their pages
+    as if they were zeros: neither the scale nor another value changes."""
+    rng = np.random.default_rng(d)
+    T = 2 * page + 5
+    m = model(rng, [T, T + 3, T], page, 2, d)
+    x, xs = storage(rng.normal(size=(3, T, 2, d)), dtype)
+    bad = rng.random(x.shape) < 0.02
+    bad[2, page:2 * page, 1] = True  # a block with no finite value
+    put = torch.from_numpy(rng.choice([math.inf, -math.inf, math.nan], x.shape)).to(dtype)
+    k = torch.where(torch.from_numpy(bad), put, x.cpu()).cuda()
+    m.write(np.where(bad, 0.0, xs), np.where(bad, 0.0, -xs))
+    c = device_cache(m)
+    clean = [t.clone() for t in (c.k, c.v, c.k_scale, c.v_scale)]
+    trevs.kv8_write(c, k, -k)
+    torch.cuda.synchronize()
+    assert torch.equal(c.k_scale, clean[2]) and torch.equal(c.v_scale, clean[3])
+    want_k, want_v = TABLE[clean[0].cpu().numpy()], TABLE[clean[1].cpu().numpy()].swapaxes(3, 4)
+    for b in range(3):
+        for t in range(T):
+            at = m.len[b] - T + t
+            p, o = m.table[b][at // page], at % page
+            want_k[0, p, :, o][bad[b, t]] = math.nan
+            want_v[0, p, :, o][bad[b, t]] = math.nan
+    assert np.array_equal(TABLE[c.k.cpu().numpy()], want_k, equal_nan=True)
+    assert np.array_equal(TABLE[c.v.cpu().numpy()].swapaxes(3, 4), want_v, equal_nan=True)
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
