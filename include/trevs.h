@@ -485,9 +485,11 @@ trevs_status trevs_kv8_write(const trevs_kv8_cache* cache, const trevs_kv8_write
  *   else:   every j < L
  *   out[b,t,h,:] = sum_j softmax_j(scale q . k_j) v_j
  *   lse[b,h,t]   = logsumexp_j(scale q . k_j), natural log
- * A row that sees no key gives zeros and -inf.  Rows t >= q_len[b] are left as
- * they were.  Products run on the matrix cores with 32-bit sums: bf16 queries
- * and attention weights as bf16, fp32 ones as three bf16 parts each. */
+ * A row that sees no key gives zeros and -inf.  A stored NaN makes the rows that
+ * see it NaN, a key's everywhere, a value's in its channel; others are as
+ * without it.  Rows t >= q_len[b] are left as they were.  Products run on the
+ * matrix cores with 32-bit sums: bf16 queries and attention weights as bf16,
+ * fp32 ones as three bf16 parts each. */
 typedef struct trevs_kv8_attention_args {
   uint32_t struct_size;      /* sizeof(trevs_kv8_attention_args) */
   int32_t B;                 /* sequences */

@@ -19,6 +19,8 @@
 // queries and weights are split into three bf16 parts, 24 bits.  (The 8-bit
 // matrix instructions would take keys unconverted, and a bf16 query as two
 // e4m3 parts, but their sums came out 2^-19 off, too far for a log-sum-exp.)
+#include <type_traits>
+
 #include "cache.hpp"
 #include "cut.hpp"
 
@@ -78,6 +80,45 @@ __device__ __forceinline__ u32x4 keep_bytes(u32x4 v, int n) {
     v[w] = k >= 4 ? v[w] : k <= 0 ? 0u : v[w] & ((1u << (8 * k)) - 1u);
   }
   return v;
+}
+
+// NaN among e4m3 values.  A row's weight for a token that it does not see is 0, which would keep the token's
+// values away from it, except that 0 NaN is NaN.  So in the steps whose tokens some rows of a tile see and others
+// do not, NaN values are multiplied as zeros; if there were any, a second pass over these steps finds the rows
+// that see them, by products of ones for NaN with ones for the tokens seen.  (Both in the main loop took its
+// registers: prompts of 4 x 4259 rows 590 -> 768 us, this way 622 -> 620.)
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {  // 1 in each byte that is NaN
+  return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+}
+// Not 0 if there is a NaN in v.
+__device__ __forceinline__ uint32_t any_nan(u32x4 v) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) any |= (v[w] & 0x7f7f7f7fu) + 0x01010101u;
+  return any & 0x80808080u;
+}
+// NaN in v set to 0; whether there was one.
+__device__ __forceinline__ bool drop_nan(u32x4& v) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const uint32_t n = nan_bytes(v[w]);
+    v[w] &= ~(n * 0xffu);
+    any |= n;
+  }
+  return any != 0;
+}
+// v as bf16, 1 where it is NaN and 0 where it is a number.
+__device__ __forceinline__ void nan_ones(u32x4 v, bf16x8 (&ones)[2]) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) v[w] = nan_bytes(v[w]) * 0x38u;  // (0x38: 1 in e4m3)
+  ones[0] = widen(v[0], v[1], 1.f);
+  ones[1] = widen(v[2], v[3], 1.f);
+}
+// A lane's 16 weights as 1 for the first n, which its row sees, and 0 for the others.
+__device__ __forceinline__ void seen_ones(int n, bf16x8 (&ones)[2]) {
+#pragma unroll
+  for (int j = 0; j < 16; ++j) ones[j >> 3][j & 7] = (__bf16)(j < n ? 1.f : 0.f);
 }
 
 template <class E>
@@ -253,6 +294,15 @@ __device__ __forceinline__ void store_lse(const AttnArgs& a, const Tile& t, int 
   a.lse[((size_t)t.b * a.H_q + h) * a.T_max + q] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
+// NaN for channel c of the staged tile's row r (counted in the group), where its output or its piece's sum is.
+template <int D>
+__device__ __forceinline__ void store_nan(const AttnArgs& a, const Piece& pc, int r, int c) {
+  if (pc.part >= 0)
+    a.part[((size_t)pc.part * kTileRows + (r - pc.t.rt * kTileRows)) * D + c] = NAN;
+  else
+    reinterpret_cast<__bf16*>(a.out)[out_row(a, pc.t, r) * D + c] = (__bf16)NAN;
+}
+
 // A workgroup takes 16 NQ rows of one group; its waves take every kWaves-th
 // step.  Nothing is staged: a lane loads its own 16 bytes of key channels and
 // of value tokens.  Bound by the cache's bytes for single tokens.
@@ -270,7 +320,8 @@ __device__ __forceinline__ u32x4 load16(const void* p) {
   return ldg16(p);
 }
 
-template <class E, int D, int NQ>
+// ONE: calls of one token a sequence, whose rows all see the same keys.
+template <class E, int D, int NQ, bool ONE>
 __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, RowsShared<E, D, NQ>& sh) {
   constexpr int NP = kParts<E>;
   constexpr int R = 16 * NQ;
@@ -328,6 +379,9 @@ __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, R
     for (int c = 0; c < D / 16; ++c) o[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
+  // some rows see tokens of a step that others do not
+  auto mixed = [&](int u) { return __any(lim_all < min(u * kStep + kStep, n_keys)); };
+  bool nan = false;  // this lane left out NaN values
   for (int u = u0 + wave; u < u1; u += kWaves) {
     const int tok = u * kStep + 16 * g4;
     const bool there = next >= 0 && next < a.c.n_pages && tok < n_keys;
@@ -369,6 +423,10 @@ __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, R
       if (!there) ks = vs = 1.f;
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) vw[c] = keep_bytes(vw[c], n_v);
+      if (!ONE && mixed(u)) {
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) nan |= drop_nan(vw[c]);
+      }
     }
     bf16x8 pw[NQ][2][NP];
 #pragma unroll
@@ -416,6 +474,30 @@ __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, R
           o[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pw[i][0][p], o[i][c], 0, 0, 0);
           o[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pw[i][1][p], o[i][c], 0, 0, 0);
         }
+    }
+  }
+  if (!ONE && __any(nan)) {
+    for (int u = u0 + wave; u < u1; u += kWaves) {
+      if (!mixed(u)) continue;
+      const int tok = u * kStep + 16 * g4, p = look_up(u);
+      const bool there = p >= 0 && p < a.c.n_pages && tok < n_keys;
+      const uint8_t* vp = v_base + (size_t)(there ? p : 0) * page_stride;
+      bf16x8 seen[NQ][2];
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) seen_ones(there ? lim[i] - tok : 0, seen[i]);
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        bf16x8 ones[2];
+        nan_ones(keep_bytes(ldg16(vp + ((size_t)(16 * c) << shift)), there ? min(max(L - tok, 0), 16) : 0), ones);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+          f32x4 hit = f32x4{0.f, 0.f, 0.f, 0.f};
+          hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones[0], seen[i][0], hit, 0, 0, 0);
+          hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones[1], seen[i][1], hit, 0, 0, 0);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[i][c][j] = hit[j] > 0.f ? NAN : o[i][c][j];
+        }
+      }
     }
   }
   // the waves' parts, in their order
@@ -478,13 +560,13 @@ __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, R
   }
 }
 
-template <class E, int D, int NQ>
+template <class E, int D, int NQ, bool ONE>
 __global__ __launch_bounds__(kWaves * 64, NQ == 1 && D <= 128 && E::kBytes == 2 ? 3 : 1) void rows_kernel(AttnArgs a) {
   __shared__ RowsShared<E, D, NQ> sh;
   Walk<16 * NQ> walk(a);
   Piece p;
   while (walk.next(a, p)) {
-    rows_piece<E, D, NQ>(a, p, sh);
+    rows_piece<E, D, NQ, ONE>(a, p, sh);
     __syncthreads();  // the sums in LDS are read before the next piece's are written
   }
 }
@@ -516,6 +598,7 @@ struct TileShared {
   static constexpr int kKeyVecs = kStep * D / 16;  // 16-byte vectors of a side
   u32x4 k[2][kKeyVecs], v[2][kKeyVecs];
   float ks[2][4], vs[2][4];  // scales of each 16 tokens; a negative key scale: absent
+  int nan[kWaves];           // whether a wave left out NaN values
 };
 
 template <int D>
@@ -590,8 +673,21 @@ __device__ __forceinline__ void tile_piece(const AttnArgs& a, const Piece& pc, T
     g_n = there ? L - (u * kStep + (tid & 3) * 16) : 0;
     if (!there) g_ks = -1.f, g_vs = 1.f;
   };
-  auto store = [&](int buf) {
+  // from this step on some rows see tokens that others do not
+  const int u_mixed = a.causal ? max(min(L - rows + r0 / a.G + 1, L), 0) / kStep : u1;
+  bool nan = false;  // this wave left out NaN values
+  auto store = [&](int buf, bool drop) {
     const bool mask = __any(g_n < 16);
+    if (drop) {
+      uint32_t found = 0;
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) found |= any_nan(gv[i]);
+      if (__any(found != 0)) {
+        nan = true;
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) drop_nan(gv[i]);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
       const int e = tid + 256 * i;
@@ -610,7 +706,7 @@ __device__ __forceinline__ void tile_piece(const AttnArgs& a, const Piece& pc, T
     look_up(u0);
     load(u0);
     look_up(u0 + 1);
-    store(0);
+    store(0, u0 >= u_mixed);
   }
   wait_vmem<0>();  // (the queries too: the loop then waits for its own loads only)
   __syncthreads();
@@ -687,12 +783,12 @@ __device__ __forceinline__ void tile_piece(const AttnArgs& a, const Piece& pc, T
         }
       }
     }
-    store(buf ^ 1);
+    if (u + 1 == u1) sh.nan[wave] = nan;
+    store(buf ^ 1, u + 1 >= u_mixed);
     __syncthreads();
   }
   l += __shfl_xor(l, 32, 64);
-  if (!live) return;
-  if (pc.part >= 0) {
+  if (live && pc.part >= 0) {
     const size_t part = (size_t)pc.part * kTileRows + 32 * wave + col;
     if (half == 0) a.part_ml[part] = make_float2(m, l);
 #pragma unroll
@@ -701,18 +797,38 @@ __device__ __forceinline__ void tile_piece(const AttnArgs& a, const Piece& pc, T
       for (int j = 0; j < 4; ++j)
         *reinterpret_cast<float4*>(a.part + part * D + 32 * c + 8 * j + 4 * half) =
             make_float4(o[c][4 * j], o[c][4 * j + 1], o[c][4 * j + 2], o[c][4 * j + 3]);
-    return;
+  } else if (live) {
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const size_t out = out_row(a, pc.t, r) * D;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float x[4] = {o[c][4 * j] * inv, o[c][4 * j + 1] * inv, o[c][4 * j + 2] * inv, o[c][4 * j + 3] * inv};
+        store4(a.out, out + 32 * c + 8 * j + 4 * half, x, BF16());
+      }
+    if (a.lse && half == 0) store_lse(a, pc.t, r, m, l);
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  const size_t out = out_row(a, pc.t, r) * D;
+  if (u0 >= u1 || !(sh.nan[0] | sh.nan[1] | sh.nan[2] | sh.nan[3])) return;
+  for (int tok = max(u0, u_mixed) * kStep + 16 * half; tok < u1 * kStep; tok += 32) {
+    const int p = tok < n_keys ? table[tok >> shift] : -1;
+    const bool there = p >= 0 && p < a.c.n_pages;
+    const uint8_t* v = a.c.v + ((size_t)(there ? p : 0) * a.c.H_kv + hk) * ((size_t)D << shift) + (tok & page_mask);
+    bf16x8 seen[2];
+    seen_ones(there ? lim - tok : 0, seen);
+    for (int c = 0; c < D / 32; ++c) {
+      bf16x8 ones[2];
+      nan_ones(keep_bytes(ldg16(v + ((size_t)(32 * c + col) << shift)), there ? L - tok : 0), ones);
+      f32x16 hit;
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c)
+      for (int i = 0; i < 16; ++i) hit[i] = 0.f;
+      hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones[0], seen[0], hit, 0, 0, 0);
+      hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones[1], seen[1], hit, 0, 0, 0);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float x[4] = {o[c][4 * j] * inv, o[c][4 * j + 1] * inv, o[c][4 * j + 2] * inv, o[c][4 * j + 3] * inv};
-      store4(a.out, out + 32 * c + 8 * j + 4 * half, x, BF16());
+      for (int i = 0; i < 16; ++i)
+        if (hit[i] > 0.f && live) store_nan<D>(a, pc, r, 32 * c + 8 * (i >> 2) + 4 * half + (i & 3));
     }
-  if (a.lse && half == 0) store_lse(a, pc.t, r, m, l);
+  }
 }
 
 template <int D>
@@ -720,7 +836,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tile_kernel(AttnArgs a)
   __shared__ TileShared<D> sh;
   Walk<kTileRows> walk(a);
   Piece p;
-  while (walk.next(a, p)) tile_piece<D>(a, p, sh);  // (a piece ends with its last reads of LDS behind a barrier)
+  // (a piece ends with its last reads of the tile behind a barrier, those of `nan` are behind the next piece's first)
+  while (walk.next(a, p)) tile_piece<D>(a, p, sh);
 }
 
 // The sums of the pieces of each cut tile joined, in the order of its steps;
@@ -800,10 +917,14 @@ hipError_t launch(AttnArgs a, const AttnPlan& p, hipStream_t s) {
       hipLaunchKernelGGL(join, dim3((unsigned)(rows / (kJoinThreads / (D / 4)))), dim3(kJoinThreads), 0, s, a);
   };
   static_assert(kWaves * 64 == 256, "one block size");
-  if (p.rows == 16) go(rows_kernel<E, D, 1>, join_kernel<E, D, 16, false>, join_kernel<E, D, 16, true>);
-  if constexpr (!(D == 256 && E::kBytes == 4)) {
-    if (p.rows == 32) go(rows_kernel<E, D, 2>, join_kernel<E, D, 32, false>, join_kernel<E, D, 32, true>);
-  }
+  auto rows = [&](auto one) {
+    constexpr bool ONE = decltype(one)::value;
+    if (p.rows == 16) go(rows_kernel<E, D, 1, ONE>, join_kernel<E, D, 16, false>, join_kernel<E, D, 16, true>);
+    if constexpr (!(D == 256 && E::kBytes == 4)) {
+      if (p.rows == 32) go(rows_kernel<E, D, 2, ONE>, join_kernel<E, D, 32, false>, join_kernel<E, D, 32, true>);
+    }
+  };
+  a.T_max == 1 ? rows(std::true_type()) : rows(std::false_type());
   if constexpr (E::kBytes == 2) {
     if (p.rows == kTileRows) go(tile_kernel<D>, join_kernel<E, D, kTileRows, false>, join_kernel<E, D, kTileRows, true>);
   }

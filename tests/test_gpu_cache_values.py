@@ -107,3 +107,60 @@ def test_attention_one_nan_key(dtype, T, loose):
         torch.cuda.synchronize()
         assert torch.isnan(out[0]).all() and torch.isnan(lse[0]).all()
         assert torch.isfinite(out[1]).all() and torch.isfinite(lse[1]).all()
+
+
+ROWS = [  # page, H_q, H_kv, d, T, len
+    (16, 3, 1, 64, 5, 40), (32, 4, 2, 128, 30, 77), (64, 7, 1, 128, 37, 300), (16, 2, 1, 256, 70, 129),
+    (32, 4, 4, 64, 200, 260),
+]
+
+
+@pytest.mark.parametrize("shape", ROWS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("loose", [False, True])
+def test_attention_nan_rows_reach_only_what_sees_them(shape, dtype, loose):
+    """Causal rows before a token whose key or value is NaN are as without it;
+    rows that see a NaN value have NaN in its channel, a NaN key in all of them
+    and in the log-sum-exp."""
+    page, H_q, H_kv, d, T, L = shape
+    print(f"[attn nan] {shape} {dtype} {loose}", flush=True)
+    rng = np.random.default_rng(L)
+    m = model(rng, [L, L], page, H_kv, d)
+    if loose:  # (cut into pieces)
+        m.table = [row + [-1] * 2000 for row in m.table]
+        m.max_pages += 2000
+    c = device_cache(m)
+    q, qs = storage(rng.normal(size=(2, T, H_q, d)), dtype)
+    call = trevs.Kv8Attention(c, q, want_lse=True)
+    call()
+    torch.cuda.synchronize()
+    out, lse = call.out.clone(), call.lse.clone()
+    G = H_q // H_kv
+    places = {L - 1, L - T, L - T + 1, L - T // 2, L - 2}
+    for at in sorted(places):
+        p, o = m.table[0][at // page], at % page
+        before_k, before_v = c.k.clone(), c.v.clone()
+        c.v[0, p, 0, 3, o] = 0x7f
+        c.v[0, p, 0, d - 1, o] = 0xff
+        call()
+        torch.cuda.synchronize()
+        t0 = at - (L - T)  # the first row that sees it
+        want = out.clone()
+        want[0, t0:, :G, 3] = math.nan
+        want[0, t0:, :G, d - 1] = math.nan
+        assert torch.equal(torch.isnan(call.out), torch.isnan(want)), at
+        ok = ~torch.isnan(want)
+        assert torch.equal(call.out[ok], want[ok]) and torch.equal(call.lse, lse), at
+        c.v.copy_(before_v)
+        c.k[0, p, 0, o, 1] = 0xff
+        call()
+        torch.cuda.synchronize()
+        want, want_lse = out.clone(), lse.clone()
+        want[0, t0:, :G] = math.nan
+        want_lse[0, :G, t0:] = math.nan
+        assert torch.equal(torch.isnan(call.out), torch.isnan(want)), at
+        assert torch.equal(torch.isnan(call.lse), torch.isnan(want_lse)), at
+        # (when sums are rescaled is the wave's choice: rows next to it may round otherwise)
+        check_attention(m, c, qs, torch.where(torch.isnan(want), out, call.out),
+                        torch.where(torch.isnan(want_lse), lse, call.lse), dtype)
+        c.k.copy_(before_k)
