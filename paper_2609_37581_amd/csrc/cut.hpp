@@ -5,17 +5,16 @@ namespace trevs {
 
 // `total` steps, those of all tiles one after the other, in n equal pieces.
 // The launch's workgroups are counted from the longest that the sequences may
-// be, `total` from what they are: n is the smaller of the launch's workgroups
-// and what gives each `side` steps (the steps that its waves take side by
-// side), so that every one of the first n has a step and the workgroups
-// between a tile's first and its last have all left their sums; the others do
-// nothing.
+// be, `total` from what they are: n is the smaller of the two, so that every
+// one of the first n has a step and the workgroups between a tile's first and
+// its last have all left their sums; the others do nothing.  (Fewer and longer
+// pieces, 4 steps for the 4 waves of a workgroup, end more often in a second
+// tile: a token of 4 sequences of 1187 under a table of 16 times that, 15.1 us,
+// and 12.2 this way.)
 struct Cut {
   int total, n;
-  __host__ __device__ __forceinline__ Cut(int total_, int workgroups, int side) : total(total_) {
-    const int most = total_ / side + (total_ % side != 0);
-    n = most < workgroups ? most : workgroups;
-  }
+  __host__ __device__ __forceinline__ Cut(int total_, int workgroups)
+      : total(total_), n(total_ < workgroups ? total_ : workgroups) {}
   // The first step of workgroup w (total for w = n).
   __host__ __device__ __forceinline__ int start(int w) const { return (int)((long long)w * total / n); }
   // The workgroup that holds a step.

@@ -211,10 +211,10 @@ struct Walk {
   Tile t;              // the tile that `at` lies in,
   Sequence seq;        // its sequence,
   int first, n;        // its first step and its steps
-  __device__ __forceinline__ explicit Walk(const AttnArgs& a) : cut(0, 0, 1), at(0), end(1) {
+  __device__ __forceinline__ explicit Walk(const AttnArgs& a) : cut(0, 0), at(0), end(1) {
     if (!a.part) return;
     s.init(a);
-    cut = Cut(s.total, gridDim.x, side_steps(R));
+    cut = Cut(s.total, gridDim.x);
     end = 0;
     if ((int)blockIdx.x >= cut.n) return;
     at = cut.start(blockIdx.x);

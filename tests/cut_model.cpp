@@ -5,7 +5,7 @@
 #include "../paper_2609_37581_amd/csrc/cut.hpp"
 
 extern "C" {
-int cut_n(int total, int workgroups, int side) { return trevs::Cut(total, workgroups, side).n; }
-int cut_start(int total, int workgroups, int side, int w) { return trevs::Cut(total, workgroups, side).start(w); }
-int cut_owner(int total, int workgroups, int side, int step) { return trevs::Cut(total, workgroups, side).owner(step); }
+int cut_n(int total, int workgroups) { return trevs::Cut(total, workgroups).n; }
+int cut_start(int total, int workgroups, int w) { return trevs::Cut(total, workgroups).start(w); }
+int cut_owner(int total, int workgroups, int step) { return trevs::Cut(total, workgroups).owner(step); }
 }

@@ -21,17 +21,17 @@ def cut(tmp_path_factory):
     return ctypes.CDLL(so)
 
 
-def replay(cut, steps, workgroups, side):
+def replay(cut, steps, workgroups):
     """`steps` of each tile that has some: the sums written (workgroup, begins a
     tile), those read for each tile, and how often each step is done."""
     total = sum(steps)
     first = np.concatenate([[0], np.cumsum(steps)])
-    n = cut.cut_n(total, workgroups, side)
+    n = cut.cut_n(total, workgroups)
     assert 0 < n <= workgroups and n <= total
     done = np.zeros(total, int)
     written, pieces, whole = set(), {}, set()
     for w in range(n):
-        at, end = cut.cut_start(total, workgroups, side, w), cut.cut_start(total, workgroups, side, w + 1)
+        at, end = cut.cut_start(total, workgroups, w), cut.cut_start(total, workgroups, w + 1)
         assert at < end
         done[at:end] += 1
         tile = int(np.searchsorted(first, at, "right")) - 1
@@ -47,11 +47,11 @@ def replay(cut, steps, workgroups, side):
             else:
                 whole.add(tile)
             if u0 == 0:
-                pieces[tile] = (w, cut.cut_owner(total, workgroups, side, int(first[tile + 1]) - 1) if part else w)
+                pieces[tile] = (w, cut.cut_owner(total, workgroups, int(first[tile + 1]) - 1) if part else w)
             at = first[tile] + u1
             tile += 1
         assert parts <= 2
-    assert cut.cut_start(total, workgroups, side, n) == total and np.all(done == 1)
+    assert cut.cut_start(total, workgroups, n) == total and np.all(done == 1)
     read = []
     for tile in range(len(steps)):
         w0, w1 = pieces[tile]
@@ -61,10 +61,10 @@ def replay(cut, steps, workgroups, side):
     assert len(read) == len(set(read)) and set(read) == written
 
 
-PLANNED = [  # steps of the tiles, workgroups launched, steps side by side
-    ([19] * 4, 300, 4), ([19] * 16, 768, 4), ([16] * 8, 768, 4), ([5] * 32, 512, 4), ([1], 768, 4), ([1], 1, 1),
-    ([19, 19, 21, 20] * 2, 210, 1), ([259] * 8 + [1] * 100, 512, 1), ([7] * 300, 512, 1), ([1] * 511, 512, 1),
-    ([1 << 20] * 40, 768, 4), ([(1 << 31) - 2], 768, 4),
+PLANNED = [  # steps of the tiles, workgroups launched
+    ([19] * 4, 300), ([19] * 16, 768), ([16] * 8, 768), ([5] * 32, 512), ([1], 768), ([1], 1),
+    ([19, 19, 21, 20] * 2, 210), ([259] * 8 + [1] * 100, 512), ([7] * 300, 512), ([1] * 511, 512),
+    ([1 << 20] * 40, 768), ([(1 << 31) - 2], 768),
 ]
 
 
@@ -77,20 +77,20 @@ def test_pieces_of_any_call(cut):
     rng = np.random.default_rng(0)
     for _ in range(300):
         steps = np.maximum(1, rng.geometric(1.0 / rng.integers(1, 40), rng.integers(1, 200))).tolist()
-        replay(cut, steps, int(rng.integers(1, 900)), int(rng.choice((1, 4))))
+        replay(cut, steps, int(rng.integers(1, 900)))
 
 
 def test_steps_up_to_31_bits(cut):
-    for steps, workgroups, side in PLANNED[-2:]:
+    for steps, workgroups in PLANNED[-2:]:
         total = sum(steps)
-        n = cut.cut_n(total, workgroups, side)
+        n = cut.cut_n(total, workgroups)
         assert n == workgroups
-        starts = [cut.cut_start(total, workgroups, side, w) for w in range(n + 1)]
+        starts = [cut.cut_start(total, workgroups, w) for w in range(n + 1)]
         assert starts == [w * total // n for w in range(n + 1)]
         for step in (0, 1, total // 3, total - 1):
-            w = cut.cut_owner(total, workgroups, side, step)
+            w = cut.cut_owner(total, workgroups, step)
             assert starts[w] <= step < starts[w + 1]
 
 
 def test_no_steps(cut):
-    assert cut.cut_n(0, 768, 4) == 0
+    assert cut.cut_n(0, 768) == 0
