@@ -940,8 +940,14 @@ AttnPlan attn_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtype, int
   p.rows = n_rows <= 16 || (d_head == 256 && !bf16) ? 16 : n_rows <= 32 || !bf16 ? 32 : kTileRows;
   p.row_tiles = (int)((n_rows + p.rows - 1) / p.rows);
   const long long tiles = (long long)B * H_kv * p.row_tiles, steps = (kv_max + kStep - 1) / kStep;
-  // workgroups that run at once, and the steps that one takes side by side
-  const int per_cu = d_head == 256 || p.rows == 32 ? 1 : p.rows == 16 && bf16 ? 3 : 2;
+  // Workgroups of a CU at once, and the steps that one takes side by side.  By their registers three kernels
+  // of 64 channels have one more than counted here, whose steps are then longer: counted as they are, calls are
+  // cut that lose by it (prompts of 4 x 2048 with 16 heads, 3 for 2: 60 -> 103 us; one token of 32 sequences of
+  // 4000, 4 for 3: 41 -> 47, in fp32, 3 for 2: 46 -> 52).  The kernel of 32 rows of 64 channels has 2, and gains
+  // by their count (24 rows of 24 sequences of 4000, 2 for 1: 47 -> 38).
+  const int per_cu = d_head == 256 ? 1
+                     : p.rows == 32 ? (bf16 && d_head == 64 ? 2 : 1)
+                     : p.rows == 16 && bf16 ? 3 : 2;
   const long long slots = 256LL * per_cu, side = side_steps(p.rows);
   // Uncut, the last round of workgroups leaves `idle` slots without a tile for as long as a tile takes
   // (a step of a workgroup: about 1.5 us, 3 in fp32); cut, a second launch joins the pieces and each piece
