@@ -4,6 +4,11 @@ Argument marshalling only: every step of both pruning stages runs in the HIP
 kernels of the library.  PyTorch supplies device memory (outputs, workspace)
 and the current stream.  If the library is missing the import of any entry
 point raises; there is no fallback path.
+
+A handle (a class here) owns its outputs and workspace, made on the stream that
+is current then: a call on another stream has to be ordered after that, and the
+handle kept until the stream is past its calls.  The one-off functions see to
+both themselves for the stream that they are given.
 """
 
 import ctypes
@@ -254,6 +259,29 @@ def _stream(stream):
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _one_off(stream, device, run, *inputs):
+    """run(), which makes a handle and calls it, on `stream` (None: torch's
+    current one).  What it allocates is that stream's memory, so a workspace
+    that is dropped on return is not taken by another stream's tensors while
+    this one still works in it; the inputs, which may be dropped too, are kept
+    from reuse until `stream` is past them, and the outputs until the caller's
+    stream is."""
+    if stream is None or stream == torch.cuda.current_stream(device):
+        return run()
+    if stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors are on {device}")
+    caller = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        out = run()
+    for t in inputs:
+        if t is not None:
+            t.record_stream(stream)
+    for t in out if isinstance(out, tuple) else (out,):
+        if t is not None:
+            t.record_stream(caller)
+    return out
+
+
 class _EventArray:
     def __init__(self, events, n_kernels):
         if events is None:
@@ -443,11 +471,15 @@ def topk_select(scores, k, stream=None):
     ascending."""
     _check(scores, "scores", scores.device, 2, torch.float32)
     B, N = scores.shape
-    out = _empty((B, k), torch.int32, scores.device)
-    st = lib().trevs_topk_select(scores.data_ptr(), B, N, k, out.data_ptr(), None, 0, _stream(stream))
-    if st:
-        raise TrevsError(st, "trevs_topk_select")
-    return out
+
+    def run():
+        out = _empty((B, k), torch.int32, scores.device)
+        st = lib().trevs_topk_select(scores.data_ptr(), B, N, k, out.data_ptr(), None, 0, _stream(None))
+        if st:
+            raise TrevsError(st, "trevs_topk_select")
+        return out
+
+    return _one_off(stream, scores.device, run, scores)
 
 
 # ---------------------------------------------------------------- diagnostics
@@ -553,7 +585,7 @@ def topk_spearman(sv, st, k, stream=None):
     """Spearman correlation of s^v and s^t within the top-k saliency set of
     each sample (Sec. 3).  sv, st [B,N] fp32 on the device.  Returns
     (rho float64 [B], kept_idx int32 [B,k] ascending)."""
-    return TopkSpearman(sv, st, k)(stream)
+    return _one_off(stream, sv.device, lambda: TopkSpearman(sv, st, k)(), sv, st)
 
 
 # ------------------------------------------------------------- serving cache
@@ -669,7 +701,7 @@ class Rope:
 
 def rope(q, k, pos, stream=None, **kw):
     """Rotary positions: returns (q_out, k_out); see Rope."""
-    return Rope(q, k, pos, **kw)(stream)
+    return _one_off(stream, q.device, lambda: Rope(q, k, pos, **kw)(), q, k, pos, kw.get("freqs"))
 
 
 class Kv8Cache:
@@ -734,7 +766,7 @@ class PagesReserve:
 
 def pages_reserve(cache, n_new, slots=None, stream=None):
     """Room for more tokens: returns (granted, copy_src, copy_dst); see PagesReserve."""
-    return PagesReserve(cache, n_new, slots)(stream)
+    return _one_off(stream, cache.device, lambda: PagesReserve(cache, n_new, slots)(), n_new, slots)
 
 
 class PagesFork:
@@ -761,7 +793,7 @@ class PagesFork:
 
 def pages_fork(cache, src, dst, n_tokens=None, stream=None):
     """Sequences that share another's pages: returns done; see PagesFork."""
-    return PagesFork(cache, src, dst, n_tokens)(stream)
+    return _one_off(stream, cache.device, lambda: PagesFork(cache, src, dst, n_tokens)(), src, dst, n_tokens)
 
 
 class PagesFree:
@@ -781,7 +813,7 @@ class PagesFree:
 
 def pages_free(cache, slots, keep=None, stream=None):
     """Pages given up; see PagesFree."""
-    PagesFree(cache, slots, keep)(stream)
+    _one_off(stream, cache.device, lambda: PagesFree(cache, slots, keep)(), slots, keep)
 
 
 class Kv8Copy:
@@ -801,7 +833,7 @@ class Kv8Copy:
 
 def kv8_copy(cache, src, dst, stream=None):
     """Pages copied in every layer; see Kv8Copy."""
-    Kv8Copy(cache, src, dst)(stream)
+    _one_off(stream, cache.device, lambda: Kv8Copy(cache, src, dst)(), src, dst)
 
 
 class Kv8Write:
@@ -830,7 +862,7 @@ class Kv8Write:
 
 def kv8_write(cache, k, v, n_new=None, slots=None, stream=None, **kw):
     """Rows written to the cache; see Kv8Write."""
-    Kv8Write(cache, k, v, n_new, slots, **kw)(stream)
+    _one_off(stream, cache.device, lambda: Kv8Write(cache, k, v, n_new, slots, **kw)(), k, v, n_new, slots)
 
 
 class Kv8Attention:
@@ -876,9 +908,13 @@ class Kv8Attention:
 def kv8_attention(cache, q, q_len=None, slots=None, stream=None, **kw):
     """Attention over the cache: returns out, or (out, lse) with want_lse=True;
     see Kv8Attention."""
-    call = Kv8Attention(cache, q, q_len, slots, **kw)
-    out = call(stream)
-    return (out, call.lse) if kw.get("want_lse") else out
+
+    def run():
+        call = Kv8Attention(cache, q, q_len, slots, **kw)
+        out = call()
+        return (out, call.lse) if kw.get("want_lse") else out
+
+    return _one_off(stream, cache.device, run, q, q_len, slots)
 
 
 class Kv8Compact:
@@ -906,7 +942,8 @@ class Kv8Compact:
 
 def kv8_compact(cache, kept_idx, src_slots, dst_slots, stream=None, **kw):
     """Kept rows of cached sequences moved together; see Kv8Compact."""
-    Kv8Compact(cache, kept_idx, src_slots, dst_slots, **kw)(stream)
+    _one_off(stream, cache.device, lambda: Kv8Compact(cache, kept_idx, src_slots, dst_slots, **kw)(),
+             kept_idx, src_slots, dst_slots)
 
 
 # ---------------------------------------------------------------- HIP events
