@@ -329,8 +329,9 @@ trevs_status trevs_topk_select(const float* scores, int32_t B, int32_t N, int32_
  * section[0] pairs use plane 0, the next section[1] plane 1, and so on.
  * Values past R are copied.  `inverse` turns by -w instead (with the same
  * attn_factor): the gradient of the rotation, and with attn_factor 1 its undoing.
- * The turns pos * freqs and their fraction are formed in 64 bits, sine and
- * cosine of the fraction in 32; positions are exact up to 2^53.
+ * The fractions of a turn are formed in 64 bits, and so are their sine and
+ * cosine, times attn_factor, for fp32 tensors, rounded once to 32 (for bf16
+ * ones in 32); positions are exact up to 2^53.
  * ---------------------------------------------------------------------- */
 #define TREVS_MAX_POS_PLANES 4
 typedef struct trevs_rope_args {

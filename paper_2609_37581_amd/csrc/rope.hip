@@ -2,7 +2,11 @@
 //
 // A pair (a, b) turns by 2 pi pos f: the turns pos * f lose what matters in
 // 32 bits (position 10^6 of a pair that turns once in 6 positions has 2^-7 of
-// a turn left), so they are reduced to a fraction of a turn in 64 bits; sine and cosine of the fraction then hold in 32.
+// a turn left), so they are reduced to a fraction of a turn in 64 bits.  For
+// fp32 rows sine and cosine are formed in 64 too and rounded once, with
+// attn_factor: the rotated values are then off by 3.7e-8, with 32-bit ones by
+// 5.6e-8 (a token of 64 sequences 4.85 us, 4.65 with those).  The rounding of
+// bf16 rows, 1.7e-3, hides either, and they take the 32-bit ones.
 //
 // Bound by bytes: every value is read and written once.  A workgroup takes a
 // few rows (tokens), forms each pair's sine and cosine once in LDS and turns
@@ -64,9 +68,16 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int rows_per
     int p = 0;
     while (p < a.n_pos - 1 && i >= a.bound[p]) ++p;
     const double at = (double)a.pos[p * a.rows + row0 + r], f = a.freqs[i];
-    float sn, cs;
-    sincospif(2.f * (float)fma(at, f, -rint(at * f)), &sn, &cs);  // (the product is not rounded)
-    turn[e] = make_float2(cs * a.attn_factor, sn * a.attn_factor * a.sign);
+    const double turns = fma(at, f, -rint(at * f));  // (the product is not rounded)
+    if constexpr (E::kBytes == 4) {
+      double sn, cs;
+      sincospi(2.0 * turns, &sn, &cs);
+      turn[e] = make_float2((float)(cs * a.attn_factor), (float)(sn * a.attn_factor * a.sign));
+    } else {
+      float sn, cs;
+      sincospif(2.f * (float)turns, &sn, &cs);
+      turn[e] = make_float2(cs * a.attn_factor, sn * a.attn_factor * a.sign);
+    }
   }
   __syncthreads();
   // items of a row: VE pairs of one head, then (out of place) the vectors past rot_dim
