@@ -489,8 +489,9 @@ trevs_status trevs_kv8_write(const trevs_kv8_cache* cache, const trevs_kv8_write
  * A row that sees no key gives zeros and -inf.  A stored NaN makes the rows that
  * see it NaN, a key's everywhere, a value's in its channel; others are as
  * without it.  Rows t >= q_len[b] are left as they were.  Products run on the
- * matrix cores with 32-bit sums: bf16 queries and attention weights as bf16,
- * fp32 ones as three bf16 parts each. */
+ * matrix cores with 32-bit sums: bf16 queries and attention weights as bf16
+ * (which adds a tenth to a quarter to the rounding error of bf16 outputs), fp32
+ * ones as three bf16 parts each. */
 typedef struct trevs_kv8_attention_args {
   uint32_t struct_size;      /* sizeof(trevs_kv8_attention_args) */
   int32_t B;                 /* sequences */

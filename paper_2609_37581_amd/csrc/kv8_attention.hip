@@ -15,7 +15,11 @@
 // e4m3 numbers are bf16 numbers, so keys and values enter the products
 // exactly.  bf16 queries do too; their calls' weights are rounded to bf16 for
 // the second product (by at most 2^-8 of each, as the output is; the sum that
-// divides them is of the unrounded ones, which the log-sum-exp needs).  fp32
+// divides them is of the unrounded ones, which the log-sum-exp needs).  That adds
+// a tenth to a quarter to the outputs' error, 1.65e-3 relative from their own
+// rounding alone: 1.82e-3 for single tokens, 1.98e-3 for questions, 2.05e-3 for
+// prompts.  (Weights in two bf16 parts would take 33 % more of a prompt's time
+// and up to 7 % of a token's.)  fp32
 // queries and weights are split into three bf16 parts, 24 bits.  (The 8-bit
 // matrix instructions would take keys unconverted, and a bf16 query as two
 // e4m3 parts, but their sums came out 2^-19 off, too far for a log-sum-exp.)
@@ -149,8 +153,8 @@ __host__ __device__ constexpr int side_steps(int rows) { return rows == kTileRow
 // steps of all of them, one after the other (sequences, row tiles, groups),
 // into equal pieces, a workgroup to a piece: a piece that covers a
 // tile finishes it, the others leave their sums to join_kernel.  (8 questions
-// over 16.5 k tokens: 225 us; groups before row tiles 238, the same with
-// neighbouring pieces on one XCD.)
+// over 16.5 k tokens took 225 us with them in this order, 238 with groups before
+// row tiles, and the same with neighbouring pieces on one XCD.)
 struct Tile {
   int b, hk, rt;
 };
@@ -325,8 +329,8 @@ template <class E, int D, int NQ, bool ONE>
 __device__ __forceinline__ void rows_piece(const AttnArgs& a, const Piece& pc, RowsShared<E, D, NQ>& sh) {
   constexpr int NP = kParts<E>;
   constexpr int R = 16 * NQ;
-  // calls of at most 16 rows a group read the cache once (64 sequences of 1.2 k to 16.5 k tokens: 125 us
-  // streamed, 132 not); of more, row tiles share it
+  // calls of at most 16 rows a group read the cache once (64 sequences of 1.2 k to 16.5 k tokens: 107 us
+  // streamed, 120 not); of more, row tiles share it
   constexpr bool kOnce = NQ == 1 && !(D == 256 && E::kBytes == 4);
   auto& s_o = sh.o;
   auto& s_m = sh.m;
@@ -574,11 +578,15 @@ __global__ __launch_bounds__(kWaves * 64, NQ == 1 && D <= 128 && E::kBytes == 2 
 // ---------------------------------------------------------------- many rows
 // A workgroup takes 128 rows of one group, its waves 32 each, and steps through
 // the keys 64 tokens at a time, staged in LDS as they are stored (8 bits) one
-// step ahead.  Prompts of 4 x 4259 rows with 28 heads of 128 take 575 to 635 us
-// (820 to 905 TFLOP/s) by the machine, a product of 8192^3 in bf16 reaches 1212.
-// The clock under load bounds both (518 us with all-zero data): logits formed
-// half a step ahead of the exponentials, operands staged as bf16 (a third fewer
-// vector instructions) and 256 rows a workgroup each took the same within 3 %.
+// step ahead.  Prompts of 4 x 4259 rows with 28 heads of 128 take 588 to 635 us
+// (820 to 885 TFLOP/s) by the machine, a product of 8192^3 in bf16 reaches 1212
+// to 1404.  Bound by the vector instructions beside the products: a wave issues
+// 368 a step (145 of them conversions, of keys and values that each of the four
+// waves widens for its own rows) to 32 products; counted over a pass, vector
+// units are busy 65 % of the cycles and matrix cores 38 %, half of that at the
+// same time.  Logits formed half a step ahead of the exponentials, operands
+// staged as bf16 (a third fewer vector instructions, twice the LDS reads) and
+// 256 rows a workgroup each took the same within 3 %.
 
 // Permutation of a staged row's 16-byte columns, by the row: 16 lanes next to
 // each other read one column of 16 rows and must meet 16 different ones modulo
@@ -844,7 +852,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void tile_kernel(AttnArgs a)
 // zeros for rows that see no key.  D / 4 threads hold a row, four channels
 // each; tiles of many pieces (MANY: 8 or more on average) give a row to a whole
 // workgroup, each D / 4 threads to every kJoinThreads / (D / 4)-th piece (one
-// sequence of 16 k tokens, 64 pieces a tile: 46.6 us without, 15.7 with).
+// sequence of 16 k tokens, 64 pieces a tile: 16.7 us without, 12.9 with).
 constexpr int kJoinThreads = 256;
 template <class E, int D, int R, bool MANY>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(AttnArgs a) {
@@ -952,12 +960,12 @@ AttnPlan attn_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtype, int
   // Uncut, the last round of workgroups leaves `idle` slots without a tile for as long as a tile takes
   // (a step of a workgroup: about 1.5 us, 3 in fp32); cut, a second launch joins the pieces and each piece
   // begins anew, about 10 us, 25 with the staged kernel's larger sums.  Measured, uncut / cut: one token of
-  // 64 sequences of 1.2 k to 16.5 k tokens, 256 tiles for 768 slots, 185 / 107 us; 8 questions over 16.5 k
-  // tokens, 224 for 512, 421 / 220; one token of 32 sequences of 4000 with 16 heads of 64, 512 for 768,
-  // 45 / 54; a prompt of 1024 rows, 224 for 512, 34 / 51; prompts of 4 x 2048 with 16 heads of 64, 1024 for
-  // 512, 65 / 154.  Calls of two rounds or more are not cut: their long tiles go first, and tiles of a group
+  // 64 sequences of 1.2 k to 16.5 k tokens, 256 tiles for 768 slots, 184 / 107 us; 8 questions over 16.5 k
+  // tokens, 224 for 512, 417 / 212; one token of 32 sequences of 4000 with 16 heads of 64, 512 for 768,
+  // 41 / 49; a prompt of 1024 rows, 224 for 512, 36 / 51; prompts of 4 x 2048 with 16 heads of 64, 1024 for
+  // 512, 64 / 142.  Calls of two rounds or more are not cut: their long tiles go first, and tiles of a group
   // that run at once share its keys in the L2, which pieces do not (prompts of 4259 rows, 3728 for 512:
-  // 590 / 1085).  The steps of all must fit 31 bits.
+  // 590 / 1093).  The steps of all must fit 31 bits.
   const long long idle = (tiles + slots - 1) / slots * slots - tiles, begin_us = p.rows == kTileRows ? 25 : 10;
   const bool cut = tiles < 2 * slots && idle * (steps / side) * (bf16 ? 3 : 6) > 2 * begin_us * slots &&
                    tiles * steps < INT32_MAX;
