@@ -522,8 +522,9 @@ trevs_status trevs_kv8_attention(const trevs_kv8_cache* cache, const trevs_kv8_a
  * src_slots[b] become the first L - K_in + n_kept tokens of slot dst_slots[b], in
  * that order, their blocks rounded to scales of their own.  Rows past
  * len[dst_slots[b]] are dropped (room is reserved before), and a sample with
- * L < P + K_in, or one slot as both, is skipped.  The slots' pages must not meet: a destination is
- * filled from pages that no destination of the call holds. */
+ * L < P + K_in, or one slot as both, is skipped.  No destination twice, and the
+ * slots' pages must not meet: a destination is filled from pages that no
+ * destination of the call holds. */
 typedef struct trevs_kv8_compact_args {
   uint32_t struct_size;      /* sizeof(trevs_kv8_compact_args) */
   int32_t B;                 /* sequences */

@@ -274,8 +274,9 @@ def _one_off(stream, device, run, *inputs):
     with torch.cuda.stream(stream):
         out = run()
     for t in inputs:
-        if t is not None:
-            t.record_stream(stream)
+        for x in t.tensors if isinstance(t, Kv8Cache) else (t,):
+            if x is not None:
+                x.record_stream(stream)
     for t in out if isinstance(out, tuple) else (out,):
         if t is not None:
             t.record_stream(caller)
@@ -734,6 +735,7 @@ class Kv8Cache:
         for t in (self.k, self.v, self.k_scale, self.v_scale, self.len, self.ref):
             t.zero_()
         self.table.fill_(-1)
+        self.tensors = (self.k, self.v, self.k_scale, self.v_scale, self.table, self.len, self.ref)
         a = Kv8CacheArgs()
         a.struct_size = ctypes.sizeof(Kv8CacheArgs)
         a.n_layers, a.n_pages, a.page_tokens, a.H_kv = n_layers, n_pages, page_tokens, H_kv
@@ -766,7 +768,7 @@ class PagesReserve:
 
 def pages_reserve(cache, n_new, slots=None, stream=None):
     """Room for more tokens: returns (granted, copy_src, copy_dst); see PagesReserve."""
-    return _one_off(stream, cache.device, lambda: PagesReserve(cache, n_new, slots)(), n_new, slots)
+    return _one_off(stream, cache.device, lambda: PagesReserve(cache, n_new, slots)(), cache, n_new, slots)
 
 
 class PagesFork:
@@ -793,7 +795,8 @@ class PagesFork:
 
 def pages_fork(cache, src, dst, n_tokens=None, stream=None):
     """Sequences that share another's pages: returns done; see PagesFork."""
-    return _one_off(stream, cache.device, lambda: PagesFork(cache, src, dst, n_tokens)(), src, dst, n_tokens)
+    return _one_off(stream, cache.device, lambda: PagesFork(cache, src, dst, n_tokens)(), cache, src, dst,
+                    n_tokens)
 
 
 class PagesFree:
@@ -813,7 +816,7 @@ class PagesFree:
 
 def pages_free(cache, slots, keep=None, stream=None):
     """Pages given up; see PagesFree."""
-    _one_off(stream, cache.device, lambda: PagesFree(cache, slots, keep)(), slots, keep)
+    _one_off(stream, cache.device, lambda: PagesFree(cache, slots, keep)(), cache, slots, keep)
 
 
 class Kv8Copy:
@@ -833,7 +836,7 @@ class Kv8Copy:
 
 def kv8_copy(cache, src, dst, stream=None):
     """Pages copied in every layer; see Kv8Copy."""
-    _one_off(stream, cache.device, lambda: Kv8Copy(cache, src, dst)(), src, dst)
+    _one_off(stream, cache.device, lambda: Kv8Copy(cache, src, dst)(), cache, src, dst)
 
 
 class Kv8Write:
@@ -862,7 +865,8 @@ class Kv8Write:
 
 def kv8_write(cache, k, v, n_new=None, slots=None, stream=None, **kw):
     """Rows written to the cache; see Kv8Write."""
-    _one_off(stream, cache.device, lambda: Kv8Write(cache, k, v, n_new, slots, **kw)(), k, v, n_new, slots)
+    _one_off(stream, cache.device, lambda: Kv8Write(cache, k, v, n_new, slots, **kw)(), cache, k, v, n_new,
+             slots)
 
 
 class Kv8Attention:
@@ -914,7 +918,7 @@ def kv8_attention(cache, q, q_len=None, slots=None, stream=None, **kw):
         out = call()
         return (out, call.lse) if kw.get("want_lse") else out
 
-    return _one_off(stream, cache.device, run, q, q_len, slots)
+    return _one_off(stream, cache.device, run, cache, q, q_len, slots)
 
 
 class Kv8Compact:
@@ -943,7 +947,7 @@ class Kv8Compact:
 def kv8_compact(cache, kept_idx, src_slots, dst_slots, stream=None, **kw):
     """Kept rows of cached sequences moved together; see Kv8Compact."""
     _one_off(stream, cache.device, lambda: Kv8Compact(cache, kept_idx, src_slots, dst_slots, **kw)(),
-             kept_idx, src_slots, dst_slots)
+             cache, kept_idx, src_slots, dst_slots)
 
 
 # ---------------------------------------------------------------- HIP events

@@ -107,6 +107,25 @@ def test_rotation_write_and_pages_on_another_stream(sizes):
     assert len(want) == len(got) and all(torch.equal(a, b) for a, b in zip(want, got))
 
 
+def test_a_cache_that_is_dropped(sizes):
+    rng = np.random.default_rng(3)
+    m = model(rng, [2000], 32, 2, 128)
+    c = device_cache(m)
+    q, _ = storage(rng.normal(size=(1, 1, 4, 128)), torch.bfloat16)
+    want = trevs.kv8_attention(c, q)
+    torch.cuda.synchronize()
+    del sizes[:]
+    c = device_cache(m)
+    taken = list(sizes)
+    side = torch.cuda.Stream()
+    behind(side)
+    out = trevs.kv8_attention(c, q, stream=side)
+    del c
+    overwrite(taken)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+
+
 def test_a_stream_of_another_device_is_refused():
     class Other:
         device = torch.device("cuda", 99)
