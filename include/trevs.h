@@ -12,8 +12,10 @@
  *     token by its max-over-text attention averaged over those heads, take a
  *     stable top-K_2, and compact hidden states, position ids and K/V rows.
  *
- * The pruned sequence then goes to a serving cache: rotary positions, a paged
- * K/V cache in 8 bits with the attention that reads it, and its pages.
+ * The pruned sequence then goes to a serving cache: rotary positions (with the
+ * norms of the heads before them), a paged K/V cache in 8 bits with the attention
+ * that reads it, and its pages.  The decode loop over it selects continuations by
+ * beam search and evicts tokens by the attention that they have had.
  *
  * Conventions for every entry point:
  *   - Tensor pointers are DEVICE pointers to dense row-major tensors.  Float
@@ -358,6 +360,28 @@ typedef struct trevs_rope_args {
 
 trevs_status trevs_rope(const trevs_rope_args* args, void* stream);
 
+/* The rotation of trevs_rope after an RMS norm of every head: with x the d_head
+ * values of one head of one row and w its weights,
+ *   y_c = x_c (mean_c x_c^2 + eps)^(-1/2) (w_c + weight_offset)
+ * is turned as trevs_rope turns (and values past rot_dim are y's).  The mean, the
+ * norm and the rotation are in 32 bits, the angles as trevs_rope has them, and the
+ * result is rounded once.  Magnitudes up to the type's largest and down to its
+ * smallest normal number keep their norm (squares that leave fp32's range are taken
+ * of scaled values).  Outputs may be the inputs, as for trevs_rope.  rope.inverse
+ * must be 0. */
+typedef struct trevs_norm_rope_args {
+  uint32_t struct_size;      /* sizeof(trevs_norm_rope_args) */
+  float eps;                 /* a normal number > 0 */
+  float weight_offset;       /* finite; 0, or 1 for weights stored as their distance from 1 */
+  int32_t weight_dtype;      /* trevs_dtype of the weights */
+  int32_t per_head;          /* 0: [d_head], for every head; 1: [H,d_head] */
+  const void* q_weight;      /* (16-byte aligned) or NULL: factors of 1, whatever weight_offset is */
+  const void* k_weight;      /* as q_weight, for k */
+  trevs_rope_args rope;      /* tensors, positions and frequencies; rope.struct_size = sizeof(trevs_rope_args) */
+} trevs_norm_rope_args;
+
+trevs_status trevs_norm_rope(const trevs_norm_rope_args* args, void* stream);
+
 /* The frequencies of trevs_rope, computed on the host into freqs [rot_dim/2]
  * (host memory): f_i = base^(-2i/rot_dim) / (2 pi) turns per position, for
  * contexts longer than the model's own divided by `factor`
@@ -537,6 +561,122 @@ typedef struct trevs_kv8_compact_args {
 
 trevs_status trevs_kv8_compact(const trevs_kv8_cache* cache, const trevs_kv8_compact_args* args, void* stream);
 
+/* Scores of cached tokens: the attention weights that they have been given.  score
+ * [n_slots, max_pages * page_tokens] holds a number for every token of every slot
+ * (the caller's; zeros for an empty slot, and past a slot's length).  One call adds
+ * the weights of one layer's query rows, all heads summed: for j < L = len[slot]
+ *   score[slot][j] = decay score[slot][j] + sum_{h, t < q_len[b], j seen by t}
+ *                    exp(scale q[b,t,h] . k_j - lse[b,h,t])
+ * with rows, keys and what they see as in trevs_kv8_attention, whose lse this is.
+ * With decay 0 what the scores held is not read, and the row is written to its end,
+ * zeros past L (a slot's first call); otherwise the row past L stays as it is.  A
+ * row whose lse is -inf gives nothing; a NaN key makes its own token's score NaN, a
+ * NaN lse those of all tokens that its row sees.  Sums are in 32 bits, in an order
+ * that the sizes of the call alone decide. */
+typedef struct trevs_kv8_weights_args {
+  uint32_t struct_size;      /* sizeof(trevs_kv8_weights_args) */
+  int32_t B;                 /* sequences */
+  int32_t T_max;             /* padded query rows, >= 1 */
+  int32_t H_q;               /* query heads; H_q % H_kv == 0 */
+  int32_t layer;             /* 0..n_layers-1 */
+  int32_t dtype;             /* trevs_dtype of q */
+  int32_t causal;            /* 0 or 1 */
+  int32_t kv_max;            /* as in trevs_kv8_attention_args: longer sequences are cut there */
+  float scale;               /* logit scale > 0, that of the attention */
+  float decay;               /* finite, >= 0: the factor of what the scores held */
+  const void* q;             /* [B,T_max,H_q,d_head], rows q_ld elements apart (16-byte aligned) */
+  int64_t q_ld;              /* 0 = H_q * d_head; row bytes % 16 == 0 */
+  const int32_t* q_len;      /* [B], clamped into 0..T_max, or NULL (= T_max) */
+  const int32_t* slots;      /* [B], or NULL (= 0..B-1, B <= n_slots); no slot twice */
+  const float* lse;          /* [B,H_q,T_max] */
+  float* score;              /* IN/OUT [n_slots, max_pages * page_tokens] */
+} trevs_kv8_weights_args;
+
+size_t trevs_kv8_weights_workspace_size(const trevs_kv8_cache* cache, const trevs_kv8_weights_args* args);
+trevs_status trevs_kv8_weights(const trevs_kv8_cache* cache, const trevs_kv8_weights_args* args, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/* Eviction by score, in every layer.  With L = len[slot] and n = keep[b] clamped
+ * into n_first + n_last..n_keep (and to 1 at least), or n_keep with keep NULL: a
+ * slot of more than n tokens keeps its first n_first, its last n_last and, of
+ * those between, the ones first under (score desc, index asc) up to n in all (NaN
+ * counts as less than any number).  The kept tokens follow each other in their
+ * order, their scores with them; scores past n become 0 and the length n.
+ * Pages before the first evicted token stay as they are, also shared with other
+ * slots.  From there on the kept rows go to free pages, the lowest ones first, in
+ * ascending order, their blocks rounded to scales of their own (rows of absent pages
+ * are zeros), and the slot gives up the pages that held them; those are free after
+ * the call, not for its later requests.  Requests are served in order; one that the
+ * free pages do not cover, that names a slot out of range or an earlier request's
+ * slot, or whose slot has no more than n tokens, changes nothing.  n_evicted[b] is
+ * L - n, or 0; kept_idx[b] lists the kept tokens' old places, ascending, then -1
+ * (-1 throughout where nothing was evicted).  The call must not run beside another
+ * one on the same cache. */
+typedef struct trevs_kv8_evict_args {
+  uint32_t struct_size;      /* sizeof(trevs_kv8_evict_args) */
+  int32_t B;                 /* requests, 1..TREVS_MAX_PAGE_REQUESTS */
+  int32_t n_keep;            /* >= 1 */
+  int32_t n_first, n_last;   /* >= 0; n_first + n_last <= n_keep */
+  const int32_t* keep;       /* OPTIONAL [B] */
+  const int32_t* slots;      /* [B], or NULL (= 0..B-1, B <= n_slots) */
+  float* score;              /* IN/OUT [n_slots, max_pages * page_tokens] */
+  int32_t* n_evicted;        /* OUT [B] */
+  int32_t* kept_idx;         /* OUT [B,n_keep] */
+} trevs_kv8_evict_args;
+
+size_t trevs_kv8_evict_workspace_size(const trevs_kv8_cache* cache, const trevs_kv8_evict_args* args);
+trevs_status trevs_kv8_evict(const trevs_kv8_cache* cache, const trevs_kv8_evict_args* args, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Beam search.  The continuations of beam w of sequence b by token v score
+ *   score[b,w] + logits[b,w,v] - logsumexp_v logits[b,w,v]
+ * and a finished beam (done[b,w] != 0) goes on by `eos` alone, with its score as it
+ * is (its logits are not read).  The n_out best of a sequence, in order (score desc,
+ * ties to the lower beam, then to the lower token), are written as score, parent
+ * (the beam) and token.  A continuation whose score is no number or +inf counts as
+ * -inf: those of a beam of score -inf (one not in use), of banned tokens (logits of
+ * -inf), of a beam with a NaN, +inf or nothing but -inf among its logits.  Where a
+ * sequence has fewer than n_out continuations the rest is (-inf, -1, -1).
+ * Exponentials and their sums are in 32 bits, everything that continuations are
+ * compared by in 64.
+ * ---------------------------------------------------------------------- */
+#define TREVS_MAX_BEAMS 64
+#define TREVS_MAX_BEAM_OUT 64
+typedef struct trevs_beam_select_args {
+  uint32_t struct_size;      /* sizeof(trevs_beam_select_args) */
+  int32_t B;                 /* sequences */
+  int32_t W;                 /* beams of each, 1..TREVS_MAX_BEAMS */
+  int32_t V;                 /* vocabulary, >= 1 */
+  int32_t n_out;             /* continuations chosen, 1..TREVS_MAX_BEAM_OUT */
+  int32_t dtype;             /* trevs_dtype of logits */
+  int32_t eos;               /* 0..V-1: the token of finished beams */
+  const void* logits;        /* [B,W,V], rows logits_ld elements apart */
+  int64_t logits_ld;         /* 0 = V */
+  const float* score;        /* [B,W] */
+  const int32_t* done;       /* OPTIONAL [B,W] */
+  float* score_out;          /* OUT [B,n_out] */
+  int32_t* parent;           /* OUT [B,n_out] */
+  int32_t* token;            /* OUT [B,n_out] */
+} trevs_beam_select_args;
+
+size_t trevs_beam_select_workspace_size(const trevs_beam_select_args* args);
+trevs_status trevs_beam_select(const trevs_beam_select_args* args, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/* The beams' sequences after a selection: slot slots[g * W + w] (slots NULL: slot
+ * g * W + w) takes over the pages and the length that slot
+ * slots[g * W + parent[g * W + w]] had before the call, for all of them at once; no
+ * page is copied (beams that share a last page get their own from
+ * trevs_pages_reserve).  With score [n_slots, max_pages * page_tokens] the tokens'
+ * scores go with them (zeros past the length).  An entry whose parent is outside
+ * 0..W-1 keeps its sequence; one whose slot is out of range or an earlier entry's
+ * does nothing, nor does one whose parent is such an entry.  W is
+ * 1..TREVS_MAX_BEAMS, n_groups * W at most TREVS_MAX_PAGE_REQUESTS.  The call must
+ * not run beside another one on the same cache. */
+trevs_status trevs_pages_reorder(const trevs_kv8_cache* cache, int32_t n_groups, int32_t W, const int32_t* slots,
+                                 const int32_t* parent, float* score, void* stream);
+
 /* Static description of a status code. */
 const char* trevs_status_string(trevs_status status);
 
@@ -553,6 +693,10 @@ size_t trevs_kv8_cache_size(void);
 size_t trevs_kv8_write_args_size(void);
 size_t trevs_kv8_attention_args_size(void);
 size_t trevs_kv8_compact_args_size(void);
+size_t trevs_norm_rope_args_size(void);
+size_t trevs_kv8_weights_args_size(void);
+size_t trevs_kv8_evict_args_size(void);
+size_t trevs_beam_select_args_size(void);
 
 #ifdef __cplusplus
 }

@@ -112,6 +112,15 @@ struct RopeArgs {
 int rope_rows(long long rows, int rot_dim);  // rows of a workgroup
 hipError_t launch_rope(const RopeArgs& a, int interleaved, int dtype, hipStream_t s);
 
+struct NormRopeArgs {
+  RopeArgs rope;
+  const void* q_weight;     // null: ones
+  const void* k_weight;
+  float eps, weight_offset;
+  int weight_bf16, per_head;
+};
+hipError_t launch_norm_rope(const NormRopeArgs& n, int interleaved, int dtype, hipStream_t s);
+
 struct WriteArgs {
   CacheView c;
   const void* k;
@@ -133,6 +142,29 @@ struct CompactArgs {
   int turns;                // others are taken in turns (0: there are none)
 };
 hipError_t launch_kv8_compact(const CompactArgs& a, int d_head, int page, hipStream_t s);
+
+// What eviction does with one request: its slot (-1: nothing), tokens before and
+// after, the first kept token that is not where it was (n: none), and the first
+// page that is given up.
+struct EvictInfo {
+  int slot, len, n, moved, first_page;
+};
+struct EvictArgs {
+  CacheView c;              // layer 0
+  int32_t* ref;
+  float* score;             // [n_slots, max_pages * page]
+  const int32_t* keep;
+  const int32_t* slots;
+  int32_t* n_evicted;
+  int32_t* kept_idx;        // [B,n_keep]
+  EvictInfo* info;          // [B]
+  int32_t* old;             // [B,max_pages] the slots' pages before
+  int B, n_keep, n_first, n_last, n_layers, page_shift;
+  int frames, turns;        // as in CompactArgs
+};
+hipError_t launch_evict_select(const EvictArgs& a, hipStream_t s);
+hipError_t launch_evict_pages(const EvictArgs& a, hipStream_t s);
+hipError_t launch_kv8_evict(const EvictArgs& a, int d_head, int page, hipStream_t s);
 
 struct CopyArgs {
   uint8_t* k;
@@ -170,6 +202,28 @@ struct AttnPlan {
 AttnPlan attn_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtype, int d_head);
 hipError_t launch_kv8_attention(const AttnArgs& a, const AttnPlan& p, int dtype, int d_head, hipStream_t s);
 
+// How the weights of a call are split: few query rows a group in one launch, many
+// into parts of (KV heads, pieces of the rows), summed by a second one.
+struct WeightsPlan {
+  bool few;
+  int key_blocks, heads, head_groups, pieces;
+};
+struct WeightsArgs {
+  CacheView c;
+  const void* q;
+  long long q_ld;           // elements
+  const int32_t* q_len;
+  const int32_t* slots;
+  const float* lse;
+  float* score;             // [n_slots,width]
+  float* part;              // [B,head_groups,pieces,kv_max]
+  int B, T_max, H_q, G, causal, kv_max, width, page_shift;
+  float scale_log2e, decay;
+  int key_blocks, heads, head_groups, pieces;
+};
+WeightsPlan weights_plan(int B, int T_max, int H_kv, int G, int kv_max);
+hipError_t launch_kv8_weights(const WeightsArgs& a, const WeightsPlan& p, int dtype, int d_head, hipStream_t s);
+
 struct PagesArgs {
   int32_t* table;
   int32_t* len;
@@ -181,6 +235,8 @@ hipError_t launch_pages_reserve(const PagesArgs& a, const int32_t* slots, const 
                                 int32_t* copy_src, int32_t* copy_dst, hipStream_t s);
 hipError_t launch_pages_fork(const PagesArgs& a, const int32_t* src, const int32_t* dst, const int32_t* n_tokens,
                              int32_t* done, hipStream_t s);
+hipError_t launch_pages_reorder(const PagesArgs& a, int groups, int width, const int32_t* slots, const int32_t* parent,
+                                float* score, hipStream_t s);
 hipError_t launch_pages_free(const PagesArgs& a, const int32_t* slots, const int32_t* keep, hipStream_t s);
 
 }  // namespace trevs

@@ -1,11 +1,13 @@
-// Host side of the serving-cache entry points: rotary positions, the 8-bit
-// paged K/V cache, its attention and its page operations.  Arguments are
-// validated before anything is launched; nothing allocates device memory or
-// waits for the device.
+// Host side of the serving-cache entry points: rotary positions and head norms,
+// the 8-bit paged K/V cache, its attention and its page operations, eviction and
+// beam search.  Arguments are validated before anything is launched; nothing
+// allocates device memory or waits for the device.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
 
+#include "beam.hpp"
 #include "cache.hpp"
 #include "host.hpp"
 
@@ -82,6 +84,62 @@ trevs_status validate_rope(const trevs_rope_args* a) {
       if (H[j] == 0) continue;
       if (!(i == j && in[i] == out[i]) && overlap(dst[i], src[j])) return TREVS_ERR_INVALID_ARG;
       if (j > i && overlap(dst[i], dst[j])) return TREVS_ERR_INVALID_ARG;
+    }
+  }
+  return TREVS_OK;
+}
+
+RopeArgs rope_args(const trevs_rope_args* a) {
+  const int e = elem_bytes(a->dtype);
+  RopeArgs r = {};
+  const void* in[2] = {a->q, a->k};
+  void* out[2] = {a->q_out, a->k_out};
+  const int H[2] = {a->H_q, a->H_k};
+  const int64_t in_ld[2] = {a->q_ld, a->k_ld}, out_ld[2] = {a->q_out_ld, a->k_out_ld};
+  for (int i = 0; i < 2; ++i) {
+    const int64_t width = (int64_t)H[i] * a->d_head;
+    r.t[i].in = reinterpret_cast<const uint8_t*>(in[i]);
+    r.t[i].out = reinterpret_cast<uint8_t*>(out[i]);
+    r.t[i].in_ld = row_ld(in_ld[i], width, e) * e;
+    r.t[i].out_ld = row_ld(out_ld[i], width, e) * e;
+    r.t[i].H = H[i];
+    r.copy_tail |= H[i] > 0 && in[i] != out[i];
+  }
+  r.freqs = a->freqs;
+  r.pos = a->pos;
+  r.rows = (long long)a->B * a->S;
+  r.d_head = a->d_head;
+  r.rot_dim = a->rot_dim;
+  r.n_pos = a->n_pos;
+  for (int p = 0, at = 0; p < a->n_pos; ++p) r.bound[p] = at += a->section[p];
+  r.attn_factor = a->attn_factor;
+  r.sign = a->inverse ? -1.f : 1.f;
+  return r;
+}
+
+trevs_status validate_norm_rope(const trevs_norm_rope_args* a) {
+  if (!a || a->struct_size != sizeof(trevs_norm_rope_args)) return TREVS_ERR_INVALID_ARG;
+  if (a->weight_dtype != TREVS_F32 && a->weight_dtype != TREVS_BF16) return TREVS_ERR_INVALID_ARG;
+  if (!(a->eps >= FLT_MIN) || !finite(a->eps) || !finite(a->weight_offset) || (a->per_head & ~1))
+    return TREVS_ERR_INVALID_ARG;
+  if (!aligned(a->q_weight, 16) || !aligned(a->k_weight, 16)) return TREVS_ERR_INVALID_ARG;
+  const trevs_rope_args* r = &a->rope;
+  TREVS_TRY(validate_rope(r));
+  if (r->inverse) return TREVS_ERR_INVALID_ARG;
+  // the weights lie outside what is written
+  const int e = elem_bytes(r->dtype), we = elem_bytes(a->weight_dtype);
+  const void* weight[2] = {a->q_weight, a->k_weight};
+  void* out[2] = {r->q_out, r->k_out};
+  const int H[2] = {r->H_q, r->H_k};
+  const int64_t out_ld[2] = {r->q_out_ld, r->k_out_ld};
+  for (int i = 0; i < 2; ++i) {
+    if (H[i] == 0) continue;
+    const int64_t width = (int64_t)H[i] * r->d_head;
+    const Rows to{out[i], (int64_t)r->B * r->S, width * e, row_ld(out_ld[i], width, e) * e};
+    for (int j = 0; j < 2; ++j) {
+      if (H[j] == 0 || !weight[j]) continue;
+      const int64_t n = (int64_t)(a->per_head ? H[j] : 1) * r->d_head;
+      if (overlap(to, Span{weight[j], (size_t)n * we})) return TREVS_ERR_INVALID_ARG;
     }
   }
   return TREVS_OK;
@@ -241,6 +299,100 @@ void plan_compact(const trevs_kv8_cache* c, const trevs_kv8_compact_args* a, Com
   t->turns = t->frames < table;
 }
 
+size_t score_bytes(const trevs_kv8_cache* c) { return (size_t)c->n_slots * c->max_pages * c->page_tokens * 4; }
+
+int weights_keys(const trevs_kv8_cache* c, const trevs_kv8_weights_args* a) {
+  return a->kv_max ? a->kv_max : c->max_pages * c->page_tokens;
+}
+WeightsPlan plan_of(const trevs_kv8_cache* c, const trevs_kv8_weights_args* a) {
+  return weights_plan(a->B, a->T_max, c->H_kv, a->H_q / c->H_kv, weights_keys(c, a));
+}
+
+trevs_status validate_weights(const trevs_kv8_cache* c, const trevs_kv8_weights_args* a) {
+  TREVS_TRY(validate_cache(c));
+  if (!a || a->struct_size != sizeof(trevs_kv8_weights_args)) return TREVS_ERR_INVALID_ARG;
+  if (a->dtype != TREVS_F32 && a->dtype != TREVS_BF16) return TREVS_ERR_INVALID_ARG;
+  if (a->B < 1 || a->T_max < 1 || a->layer < 0 || a->layer >= c->n_layers) return TREVS_ERR_INVALID_ARG;
+  if (a->H_q < 1 || a->H_q % c->H_kv || (a->causal & ~1)) return TREVS_ERR_INVALID_ARG;
+  if (a->kv_max < 0 || a->kv_max > c->max_pages * c->page_tokens) return TREVS_ERR_INVALID_ARG;
+  if (!finite(a->scale) || a->scale <= 0.f || !finite(a->decay) || a->decay < 0.f) return TREVS_ERR_INVALID_ARG;
+  if (a->B > c->n_slots) return TREVS_ERR_INVALID_ARG;  // (no slot twice)
+  const int e = elem_bytes(a->dtype);
+  const int64_t width = (int64_t)a->H_q * c->d_head, rows = (int64_t)a->B * a->T_max;
+  const int64_t ql = row_ld(a->q_ld, width, e);
+  if (!a->q || !a->lse || !a->score || !aligned(a->q, 16) || !aligned(a->lse, 4) || !aligned(a->score, 4) || !ql)
+    return TREVS_ERR_INVALID_ARG;
+  if (!aligned(a->q_len, 4) || !aligned(a->slots, 4)) return TREVS_ERR_INVALID_ARG;
+  if (a->H_q > 1024 || rows * a->H_q > INT32_MAX - 1024 || a->B > 65535) return TREVS_ERR_UNSUPPORTED;
+  const Rows q{a->q, rows, width * e, ql * e};
+  const Span score{a->score, score_bytes(c)};
+  const Span in[] = {q.span(), {a->q_len, a->q_len ? (size_t)a->B * 4 : 0}, {a->slots, a->slots ? (size_t)a->B * 4 : 0},
+                     {a->lse, (size_t)(rows * a->H_q * 4)}};
+  if (any_overlap(&score, 1, in, 4) || meets_cache(c, score)) return TREVS_ERR_INVALID_ARG;
+  const WeightsPlan p = plan_of(c, a);
+  const int64_t groups = (int64_t)a->B * p.head_groups * p.key_blocks;
+  if (p.few ? (int64_t)a->B * p.key_blocks > kMaxGroups / 4 : groups > kMaxGroups / p.pieces) return TREVS_ERR_UNSUPPORTED;
+  return TREVS_OK;
+}
+size_t weights_bytes(const trevs_kv8_cache* c, const trevs_kv8_weights_args* a) {
+  const WeightsPlan p = plan_of(c, a);
+  if (p.few) return kWsAlign;
+  return align_up((size_t)a->B * p.head_groups * p.pieces * weights_keys(c, a) * sizeof(float));
+}
+
+trevs_status validate_evict(const trevs_kv8_cache* c, const trevs_kv8_evict_args* a) {
+  TREVS_TRY(validate_cache(c));
+  if (!a || a->struct_size != sizeof(trevs_kv8_evict_args)) return TREVS_ERR_INVALID_ARG;
+  if (a->B < 1 || a->n_keep < 1 || a->n_first < 0 || a->n_last < 0 || (int64_t)a->n_first + a->n_last > a->n_keep)
+    return TREVS_ERR_INVALID_ARG;
+  if (!a->score || !a->n_evicted || !a->kept_idx) return TREVS_ERR_INVALID_ARG;
+  if (!aligned(a->score, 4) || !aligned(a->n_evicted, 4) || !aligned(a->kept_idx, 4) || !aligned(a->keep, 4) ||
+      !aligned(a->slots, 4))
+    return TREVS_ERR_INVALID_ARG;
+  if (!a->slots && a->B > c->n_slots) return TREVS_ERR_INVALID_ARG;
+  if (a->B > TREVS_MAX_PAGE_REQUESTS) return TREVS_ERR_UNSUPPORTED;
+  if ((int64_t)a->B * a->n_keep > INT32_MAX) return TREVS_ERR_UNSUPPORTED;
+  if ((int64_t)c->n_layers * a->B * c->H_kv + a->B > kMaxGroups) return TREVS_ERR_UNSUPPORTED;
+  const size_t list = (size_t)a->B * 4;
+  const Span out[] = {{a->score, score_bytes(c)}, {a->n_evicted, list}, {a->kept_idx, list * a->n_keep}};
+  const Span in[] = {{a->keep, a->keep ? list : 0}, {a->slots, a->slots ? list : 0}};
+  if (any_overlap(out, 3, in, 2)) return TREVS_ERR_INVALID_ARG;
+  for (const Span& x : out)
+    if (meets_cache(c, x)) return TREVS_ERR_INVALID_ARG;
+  for (const Span& x : in)
+    if (meets_cache(c, x)) return TREVS_ERR_INVALID_ARG;
+  return TREVS_OK;
+}
+size_t evict_info_bytes(const trevs_kv8_evict_args* a) { return align_up((size_t)a->B * sizeof(EvictInfo)); }
+
+// ---------------------------------------------------------------- beam search
+int beam_chunks(const trevs_beam_select_args* a) { return (int)(((int64_t)a->V + kBeamChunk - 1) / kBeamChunk); }
+
+trevs_status validate_beam(const trevs_beam_select_args* a) {
+  if (!a || a->struct_size != sizeof(trevs_beam_select_args)) return TREVS_ERR_INVALID_ARG;
+  if (a->dtype != TREVS_F32 && a->dtype != TREVS_BF16) return TREVS_ERR_INVALID_ARG;
+  if (a->B < 1 || a->W < 1 || a->V < 1 || a->n_out < 1 || a->eos < 0 || a->eos >= a->V) return TREVS_ERR_INVALID_ARG;
+  if (a->logits_ld != 0 && a->logits_ld < a->V) return TREVS_ERR_INVALID_ARG;
+  const int e = elem_bytes(a->dtype);
+  if (!a->logits || !a->score || !a->score_out || !a->parent || !a->token) return TREVS_ERR_INVALID_ARG;
+  if (!aligned(a->logits, e) || !aligned(a->score, 4) || !aligned(a->done, 4) || !aligned(a->score_out, 4) ||
+      !aligned(a->parent, 4) || !aligned(a->token, 4))
+    return TREVS_ERR_INVALID_ARG;
+  if (a->W > TREVS_MAX_BEAMS || a->n_out > TREVS_MAX_BEAM_OUT || a->logits_ld > INT32_MAX) return TREVS_ERR_UNSUPPORTED;
+  if ((int64_t)a->W * a->V > INT32_MAX || (int64_t)a->B * a->W > INT32_MAX) return TREVS_ERR_UNSUPPORTED;
+  const int64_t rows = (int64_t)a->B * a->W, ld = a->logits_ld ? a->logits_ld : a->V;
+  if (rows > kMaxGroups / beam_chunks(a) || a->B > kMaxGroups / 4) return TREVS_ERR_UNSUPPORTED;
+  const size_t list = (size_t)a->B * a->n_out * 4;
+  const Span out[] = {{a->score_out, list}, {a->parent, list}, {a->token, list}};
+  const Span in[] = {{a->logits, (size_t)((rows - 1) * ld + a->V) * e}, {a->score, (size_t)rows * 4},
+                     {a->done, a->done ? (size_t)rows * 4 : 0}};
+  if (any_overlap(out, 3, in, 3)) return TREVS_ERR_INVALID_ARG;
+  return TREVS_OK;
+}
+size_t beam_part_bytes(const trevs_beam_select_args* a) {
+  return align_up((size_t)a->B * a->W * beam_chunks(a) * sizeof(float2));
+}
+
 }  // namespace
 
 extern "C" {
@@ -250,6 +402,10 @@ size_t trevs_kv8_cache_size(void) { return sizeof(trevs_kv8_cache); }
 size_t trevs_kv8_write_args_size(void) { return sizeof(trevs_kv8_write_args); }
 size_t trevs_kv8_attention_args_size(void) { return sizeof(trevs_kv8_attention_args); }
 size_t trevs_kv8_compact_args_size(void) { return sizeof(trevs_kv8_compact_args); }
+size_t trevs_norm_rope_args_size(void) { return sizeof(trevs_norm_rope_args); }
+size_t trevs_kv8_weights_args_size(void) { return sizeof(trevs_kv8_weights_args); }
+size_t trevs_kv8_evict_args_size(void) { return sizeof(trevs_kv8_evict_args); }
+size_t trevs_beam_select_args_size(void) { return sizeof(trevs_beam_select_args); }
 
 trevs_status trevs_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double original_len,
                                     double beta_fast, double beta_slow, double* freqs) {
@@ -273,31 +429,21 @@ trevs_status trevs_rope_frequencies(int32_t rot_dim, double base, int32_t scalin
 
 trevs_status trevs_rope(const trevs_rope_args* a, void* stream) {
   TREVS_TRY(validate_rope(a));
-  const int e = elem_bytes(a->dtype);
-  RopeArgs r = {};
-  const void* in[2] = {a->q, a->k};
-  void* out[2] = {a->q_out, a->k_out};
-  const int H[2] = {a->H_q, a->H_k};
-  const int64_t in_ld[2] = {a->q_ld, a->k_ld}, out_ld[2] = {a->q_out_ld, a->k_out_ld};
-  for (int i = 0; i < 2; ++i) {
-    const int64_t width = (int64_t)H[i] * a->d_head;
-    r.t[i].in = reinterpret_cast<const uint8_t*>(in[i]);
-    r.t[i].out = reinterpret_cast<uint8_t*>(out[i]);
-    r.t[i].in_ld = row_ld(in_ld[i], width, e) * e;
-    r.t[i].out_ld = row_ld(out_ld[i], width, e) * e;
-    r.t[i].H = H[i];
-    r.copy_tail |= H[i] > 0 && in[i] != out[i];
-  }
-  r.freqs = a->freqs;
-  r.pos = a->pos;
-  r.rows = (long long)a->B * a->S;
-  r.d_head = a->d_head;
-  r.rot_dim = a->rot_dim;
-  r.n_pos = a->n_pos;
-  for (int p = 0, at = 0; p < a->n_pos; ++p) r.bound[p] = at += a->section[p];
-  r.attn_factor = a->attn_factor;
-  r.sign = a->inverse ? -1.f : 1.f;
-  TREVS_HIP(launch_rope(r, a->interleaved, a->dtype, reinterpret_cast<hipStream_t>(stream)));
+  TREVS_HIP(launch_rope(rope_args(a), a->interleaved, a->dtype, reinterpret_cast<hipStream_t>(stream)));
+  return TREVS_OK;
+}
+
+trevs_status trevs_norm_rope(const trevs_norm_rope_args* a, void* stream) {
+  TREVS_TRY(validate_norm_rope(a));
+  NormRopeArgs n;
+  n.rope = rope_args(&a->rope);
+  n.q_weight = a->q_weight;
+  n.k_weight = a->k_weight;
+  n.eps = a->eps;
+  n.weight_offset = a->weight_offset;
+  n.weight_bf16 = a->weight_dtype == TREVS_BF16;
+  n.per_head = a->per_head;
+  TREVS_HIP(launch_norm_rope(n, a->rope.interleaved, a->rope.dtype, reinterpret_cast<hipStream_t>(stream)));
   return TREVS_OK;
 }
 
@@ -432,6 +578,125 @@ trevs_status trevs_kv8_compact(const trevs_kv8_cache* c, const trevs_kv8_compact
   t.n_layers = c->n_layers;
   plan_compact(c, a, &t);
   TREVS_HIP(launch_kv8_compact(t, c->d_head, c->page_tokens, reinterpret_cast<hipStream_t>(stream)));
+  return TREVS_OK;
+}
+
+size_t trevs_kv8_weights_workspace_size(const trevs_kv8_cache* c, const trevs_kv8_weights_args* a) {
+  if (validate_weights(c, a) != TREVS_OK) return 0;
+  return weights_bytes(c, a);
+}
+
+trevs_status trevs_kv8_weights(const trevs_kv8_cache* c, const trevs_kv8_weights_args* a, void* ws, size_t ws_bytes,
+                               void* stream) {
+  TREVS_TRY(validate_weights(c, a));
+  TREVS_TRY(check_ws(ws, ws_bytes, weights_bytes(c, a)));
+  const WeightsPlan p = plan_of(c, a);
+  WeightsArgs t;
+  t.c = layer_view(*c, a->layer);
+  t.q = a->q;
+  t.q_ld = a->q_ld ? a->q_ld : (int64_t)a->H_q * c->d_head;
+  t.q_len = a->q_len;
+  t.slots = a->slots;
+  t.lse = a->lse;
+  t.score = a->score;
+  t.part = reinterpret_cast<float*>(ws);
+  t.B = a->B;
+  t.T_max = a->T_max;
+  t.H_q = a->H_q;
+  t.G = a->H_q / c->H_kv;
+  t.causal = a->causal;
+  t.kv_max = weights_keys(c, a);
+  t.width = c->max_pages * c->page_tokens;
+  t.page_shift = page_shift(c);
+  t.scale_log2e = a->scale * kLog2e;
+  t.decay = a->decay;
+  t.key_blocks = p.key_blocks;
+  t.heads = p.heads;
+  t.head_groups = p.head_groups;
+  t.pieces = p.pieces;
+  TREVS_HIP(launch_kv8_weights(t, p, a->dtype, c->d_head, reinterpret_cast<hipStream_t>(stream)));
+  return TREVS_OK;
+}
+
+size_t trevs_kv8_evict_workspace_size(const trevs_kv8_cache* c, const trevs_kv8_evict_args* a) {
+  if (validate_evict(c, a) != TREVS_OK) return 0;
+  return evict_info_bytes(a) + align_up((size_t)a->B * c->max_pages * sizeof(int32_t));
+}
+
+trevs_status trevs_kv8_evict(const trevs_kv8_cache* c, const trevs_kv8_evict_args* a, void* ws, size_t ws_bytes,
+                             void* stream) {
+  TREVS_TRY(validate_evict(c, a));
+  TREVS_TRY(check_ws(ws, ws_bytes, trevs_kv8_evict_workspace_size(c, a)));
+  EvictArgs t;
+  t.c = layer_view(*c, 0);
+  t.ref = c->ref;
+  t.score = a->score;
+  t.keep = a->keep;
+  t.slots = a->slots;
+  t.n_evicted = a->n_evicted;
+  t.kept_idx = a->kept_idx;
+  t.info = reinterpret_cast<EvictInfo*>(ws);
+  t.old = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(ws) + evict_info_bytes(a));
+  t.B = a->B;
+  t.n_keep = a->n_keep;
+  t.n_first = a->n_first;
+  t.n_last = a->n_last;
+  t.n_layers = c->n_layers;
+  t.page_shift = page_shift(c);
+  // a workgroup for every block that the kept tokens can fill, or as many as a launch holds, taken in turns
+  const int64_t each = (int64_t)c->n_layers * a->B * c->H_kv, page = c->page_tokens;
+  const int64_t blocks = std::min(((int64_t)a->n_keep + page - 1) / page, (int64_t)c->max_pages);
+  t.frames = (int)std::min(blocks, (kMaxGroups - a->B) / each);
+  t.turns = t.frames < blocks;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  TREVS_HIP(launch_evict_select(t, s));
+  TREVS_HIP(launch_evict_pages(t, s));
+  TREVS_HIP(launch_kv8_evict(t, c->d_head, c->page_tokens, s));
+  return TREVS_OK;
+}
+
+trevs_status trevs_pages_reorder(const trevs_kv8_cache* c, int32_t n_groups, int32_t W, const int32_t* slots,
+                                 const int32_t* parent, float* score, void* stream) {
+  TREVS_TRY(validate_cache(c));
+  if (n_groups < 1 || W < 1 || !parent) return TREVS_ERR_INVALID_ARG;
+  if (!aligned(slots, 4) || !aligned(parent, 4) || !aligned(score, 4)) return TREVS_ERR_INVALID_ARG;
+  const int64_t n = (int64_t)n_groups * W;
+  if (!slots && n > c->n_slots) return TREVS_ERR_INVALID_ARG;
+  if (W > TREVS_MAX_BEAMS || n > TREVS_MAX_PAGE_REQUESTS) return TREVS_ERR_UNSUPPORTED;
+  const Span in[] = {{slots, slots ? (size_t)n * 4 : 0}, {parent, (size_t)n * 4}};
+  const Span out{score, score ? score_bytes(c) : 0};
+  if (any_overlap(&out, 1, in, 2) || meets_cache(c, out) || meets_cache(c, in[0]) || meets_cache(c, in[1]))
+    return TREVS_ERR_INVALID_ARG;
+  TREVS_HIP(launch_pages_reorder(pages_args(c, (int)n), n_groups, W, slots, parent, score,
+                                 reinterpret_cast<hipStream_t>(stream)));
+  return TREVS_OK;
+}
+
+size_t trevs_beam_select_workspace_size(const trevs_beam_select_args* a) {
+  if (validate_beam(a) != TREVS_OK) return 0;
+  return beam_part_bytes(a) + align_up((size_t)a->B * a->W * beam_chunks(a) * a->n_out * sizeof(uint64_t));
+}
+
+trevs_status trevs_beam_select(const trevs_beam_select_args* a, void* ws, size_t ws_bytes, void* stream) {
+  TREVS_TRY(validate_beam(a));
+  TREVS_TRY(check_ws(ws, ws_bytes, trevs_beam_select_workspace_size(a)));
+  BeamArgs t;
+  t.logits = a->logits;
+  t.ld = a->logits_ld ? a->logits_ld : a->V;
+  t.score = a->score;
+  t.done = a->done;
+  t.score_out = a->score_out;
+  t.parent = a->parent;
+  t.token = a->token;
+  t.part = reinterpret_cast<float2*>(ws);
+  t.cand = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(ws) + beam_part_bytes(a));
+  t.B = a->B;
+  t.W = a->W;
+  t.V = a->V;
+  t.n = a->n_out;
+  t.eos = a->eos;
+  t.chunks = beam_chunks(a);
+  TREVS_HIP(launch_beam_select(t, a->dtype, reinterpret_cast<hipStream_t>(stream)));
   return TREVS_OK;
 }
 

@@ -1,0 +1,125 @@
+// Which tokens of a cached sequence stay: the first and last ones, and of those
+// between the highest scores.
+//
+// One workgroup to a sequence: the choice is a stable top-K (select.hpp) over keys
+// held in registers, E of them a thread, in which the tokens that always stay have
+// the largest key and NaN the smallest.  Bound by latency: the selection's passes
+// over LDS histograms, one after the other.  Sequences longer than its 65,536
+// tokens take a bisection over the keys' bits that reads the scores again each time.
+#include "cache.hpp"
+#include "select.hpp"
+
+namespace trevs {
+namespace {
+
+__device__ __forceinline__ uint32_t score_key(float s) { return s != s ? 0u : f2key(s); }
+
+// Calls emit(j, kept, kept tokens before j) for every token j < L, n < L of which are kept.
+template <int E, class Emit>
+__device__ __forceinline__ void select_held(const float* score, int L, int n, int first, int last, Emit emit,
+                                            SelectShared& sh) {
+  uint32_t key[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int j = e * kSelThreads + (int)threadIdx.x;
+    key[e] = score_key(score[min(j, L - 1)]);
+    if (j < first || j >= L - last) key[e] = 0xffffffffu;
+  }
+  block_topk_each<E>(
+      key, L, n,
+      [&](int e, bool ok, bool keep, int before) {
+        if (ok) emit(e * kSelThreads + (int)threadIdx.x, keep, before);
+      },
+      sh, false, 0u, 0u);
+}
+
+// The same for any length: a thread owns `per` tokens in a row.
+template <class Emit>
+__device__ void select_streamed(const float* score, int L, int n, int first, int last, Emit emit, SelectShared& sh) {
+  const int per = (L + kSelThreads - 1) / kSelThreads;
+  const int j0 = (int)min((long long)threadIdx.x * per, (long long)L), j1 = min(j0 + per, L);
+  auto key = [&](int j) { return j < first || j >= L - last ? 0xffffffffu : score_key(score[j]); };
+  auto count = [&](uint32_t least) {
+    int c = 0, total;
+    for (int j = j0; j < j1; ++j) c += key(j) >= least;
+    block_excl_scan(c, sh, total);
+    return total;
+  };
+  uint32_t thr = 0;  // the n-th largest key
+  for (int bit = 31; bit >= 0; --bit)
+    if (count(thr | (1u << bit)) >= n) thr |= 1u << bit;
+  int above = 0, ties = 0, n_above, n_ties;
+  for (int j = j0; j < j1; ++j) {
+    const uint32_t k = key(j);
+    above += k > thr;
+    ties += k == thr;
+  }
+  above = block_excl_scan(above, sh, n_above);
+  ties = block_excl_scan(ties, sh, n_ties);
+  const int need = n - n_above;
+  for (int j = j0; j < j1; ++j) {
+    const uint32_t k = key(j);
+    emit(j, k > thr || (k == thr && ties < need), above + min(ties, need));
+    above += k > thr;
+    ties += k == thr;
+  }
+}
+
+__global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) {
+  __shared__ SelectShared sh;
+  __shared__ int s_first;
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const int slot = slot_of(a.slots, b, a.c.n_slots);
+  bool bad = slot < 0;
+  if (a.slots)
+    for (int j = tid; j < b; j += kSelThreads) bad = bad || a.slots[j] == slot;
+  if (tid == 0) s_first = INT32_MAX;
+  int32_t* kept = a.kept_idx + (size_t)b * a.n_keep;
+  const int L = slot_len(a.c.len, slot, a.c.max_pages << a.page_shift);
+  const int least = max(a.n_first + a.n_last, 1);
+  const int n = a.keep ? min(max(a.keep[b], least), a.n_keep) : a.n_keep;
+  if (__syncthreads_or(bad) || L <= n) {
+    for (int i = tid; i < a.n_keep; i += kSelThreads) kept[i] = -1;
+    if (tid == 0) a.info[b] = EvictInfo{-1, 0, 0, 0, 0};
+    return;
+  }
+  const float* score = a.score + ((size_t)slot * a.c.max_pages << a.page_shift);
+  int gone = INT32_MAX;  // this thread's first evicted token
+  auto emit = [&](int j, bool keep, int before) {
+    if (!keep)
+      gone = min(gone, j);
+    else if (before < n)  // (exactly n are kept; the bound guards memory)
+      kept[before] = j;
+  };
+  if (L <= 1 * kSelThreads)
+    select_held<1>(score, L, n, a.n_first, a.n_last, emit, sh);
+  else if (L <= 4 * kSelThreads)
+    select_held<4>(score, L, n, a.n_first, a.n_last, emit, sh);
+  else if (L <= 16 * kSelThreads)
+    select_held<16>(score, L, n, a.n_first, a.n_last, emit, sh);
+  else if (L <= 32 * kSelThreads)
+    select_held<32>(score, L, n, a.n_first, a.n_last, emit, sh);
+  else if (L <= TREVS_MAX_SELECT_N)
+    select_held<64>(score, L, n, a.n_first, a.n_last, emit, sh);
+  else
+    select_streamed(score, L, n, a.n_first, a.n_last, emit, sh);
+  if (gone != INT32_MAX) atomicMin(&s_first, gone);
+  for (int i = n + tid; i < a.n_keep; i += kSelThreads) kept[i] = -1;
+  __syncthreads();
+  // tokens before the first evicted one stay where they are: kept[i] = i below it, and above i from there on
+  const int moved = min(s_first, n);
+  const int page = 1 << a.page_shift, want = (n + page - 1) >> a.page_shift;
+  const int from = moved < n ? moved >> a.page_shift : want;
+  for (int j = from + tid; j < (L + page - 1) >> a.page_shift; j += kSelThreads)
+    a.old[(size_t)b * a.c.max_pages + j] = a.c.table[(size_t)slot * a.c.max_pages + j];
+  if (tid == 0) a.info[b] = EvictInfo{slot, L, n, moved, from};
+}
+
+}  // namespace
+
+hipError_t launch_evict_select(const EvictArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(evict_select_kernel, dim3(a.B), dim3(kSelThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace trevs

@@ -191,11 +191,156 @@ struct TokenMap {
   u32x4 at[PAGE / 16];  // a byte a token
 };
 
-// Block (layer, b, f, h) of a destination, gathered from the source's rows.
-// Values lie token last, a byte of each channel apart: a workgroup brings each
-// source block that its tokens name into LDS whole, 16 bytes a lane, and takes
-// the bytes from there (single bytes from memory, a line each: 37.5 us for 4
+// A destination block filled from rows of others: token t < hi from row at[t] of
+// source block from[t] (-1: zeros), given by thread t; keys or values of KV head h
+// in one layer.  Values lie token last, a byte of each channel apart: a workgroup
+// brings each source block that its tokens name into LDS whole, 16 bytes a lane, and
+// takes the bytes from there (single bytes from memory, a line each: 37.5 us for 4
 // layers of 4 x 1187 of 4259 tokens, this way 20).
+template <int D, int PAGE>
+struct MoveShared {
+  uint32_t lds[D * Block<D, PAGE>::kRow];
+  float red[4];
+  TokenMap<PAGE> map;
+  uint64_t runs;
+};
+template <int D, int PAGE>
+__device__ __forceinline__ void move_block(const CacheView& v, int layer, int h, bool values, int page, int from, int at,
+                                           int hi, MoveShared<D, PAGE>& sh) {
+  using B = Block<D, PAGE>;
+  const int tid = threadIdx.x;
+  auto& lds = sh.lds;
+  auto& red = sh.red;
+  auto& map = sh.map;
+  if (tid >= hi) from = -1;
+  const size_t layer_blocks = (size_t)layer * v.n_pages * v.H_kv;
+  const uint8_t* data = (values ? v.v : v.k) + (layer_blocks + h) * (PAGE * D);
+  const float* scales = (values ? v.v_scale : v.k_scale) + layer_blocks + h;
+  if (tid < 64) {
+    if (tid < PAGE) {
+      map.block[tid] = from;
+      reinterpret_cast<uint8_t*>(map.at)[tid] = (uint8_t)at;
+      map.scale[tid] = from >= 0 ? scales[(size_t)from * v.H_kv] : 0.f;
+    }
+    const int before = __shfl_up(from, 1, 64);
+    const uint64_t starts = __ballot(tid < hi && (tid == 0 || from != before));
+    if (tid == 0) sh.runs = starts;  // tokens whose page is not the one before's
+  }
+  __syncthreads();
+  const size_t block = layer_blocks + (size_t)page * v.H_kv + h;
+  if (!values) {
+    float x[B::kPer][4][8], m = 0.f;
+#pragma unroll
+    for (int u = 0; u < B::kPer; ++u) {
+      const int e = tid + u * B::kThreads;
+      const int c = e % (D / 8) * 8, t0 = e / (D / 8) * 4;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = t0 + i;
+        const int from = t < hi ? map.block[t] : -1;
+        const int row = reinterpret_cast<const uint8_t*>(map.at)[t];
+        const u32x2 w = from >= 0 ? *reinterpret_cast<const u32x2*>(data + (size_t)from * v.H_kv * (PAGE * D) +
+                                                                    row * D + c)
+                                  : u32x2{0u, 0u};
+        float y[2][4];
+        from_e4m3(w[0], y[0]);
+        from_e4m3(w[1], y[1]);
+        const float s = from >= 0 ? map.scale[t] : 0.f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          x[u][i][q] = y[q >> 2][q & 3] * s;
+          m = fmaxf(m, fabsf(x[u][i][q]));
+        }
+      }
+    }
+    const float s = block_scale(block_max<B::kThreads>(m, red));
+    store_block<D, PAGE>(v.k + block * (PAGE * D), false, 0, hi, pow2_inverse(s), 1.f, x, lds);
+    if (tid == 0) v.k_scale[block] = s;
+  } else {
+    // a thread's items: 16 tokens of a channel, as bytes
+    constexpr int kGroups = PAGE / 16, kItems = D * kGroups / B::kThreads;
+    static_assert(kItems * B::kThreads == D * kGroups, "whole items");
+    u32x4 w[kItems], next[kItems], at16[kItems];
+    uint64_t runs = sh.runs;
+    auto fetch = [&](int t) {
+      const int from = map.block[t];
+#pragma unroll
+      for (int i = 0; i < kItems; ++i)
+        next[i] = from >= 0 ? ldg16(data + (size_t)from * v.H_kv * (PAGE * D) + (tid + i * B::kThreads) * 16)
+                            : zero4();
+    };
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      w[i] = zero4();
+      at16[i] = map.at[(tid + i * B::kThreads) % kGroups];
+    }
+    int r0 = 0;
+    fetch(0);
+    while (r0 < hi) {
+      runs &= runs - 1;
+      const int r1 = runs ? __builtin_ctzll(runs) : hi;
+#pragma unroll
+      for (int i = 0; i < kItems; ++i) {
+        const int e = tid + i * B::kThreads;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) lds[e / kGroups * B::kRow + e % kGroups * 4 + j] = next[i][j];
+      }
+      __syncthreads();
+      if (r1 < hi) fetch(r1);
+#pragma unroll
+      for (int i = 0; i < kItems; ++i) {
+        const int e = tid + i * B::kThreads, t0 = e % kGroups * 16;
+        const uint8_t* row = reinterpret_cast<const uint8_t*>(lds + e / kGroups * B::kRow);
+        // a byte for every token, those of other blocks dropped: the reads wait for nothing
+        uint32_t byte[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) byte[j] = row[(at16[i][j >> 2] >> (8 * (j & 3))) & 0xff];
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          w[i][j >> 2] |= t0 + j >= r0 && t0 + j < r1 ? byte[j] << (8 * (j & 3)) : 0u;
+      }
+      __syncthreads();
+      r0 = r1;
+    }
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const int t0 = (tid + i * B::kThreads) % kGroups * 16;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float y[4];
+        from_e4m3(w[i][j], y);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) m = fmaxf(m, fabsf(y[q]) * map.scale[t0 + 4 * j + q]);
+      }
+    }
+    const float s = block_scale(block_max<B::kThreads>(m, red)), inv = pow2_inverse(s);
+    uint8_t* out = v.v + block * (PAGE * D);
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const int e = tid + i * B::kThreads, t0 = e % kGroups * 16;
+      if (t0 >= hi) continue;
+      u32x4* to = reinterpret_cast<u32x4*>(out + e * 16);
+      u32x4 y = t0 + 16 > hi ? *to : zero4();  // tokens past the last are kept
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float x[4];
+        from_e4m3(w[i][j], x);
+#pragma unroll
+        // (one factor after the other: a block of zeros has the smallest scale, and the product of the two
+        // passes fp32's range)
+        for (int q = 0; q < 4; ++q) x[q] = x[q] * map.scale[t0 + 4 * j + q] * inv;
+        const int n_t = hi - t0 - 4 * j;  // tokens of this word
+        const uint32_t mask = n_t >= 4 ? ~0u : n_t <= 0 ? 0u : (1u << (8 * n_t)) - 1u;
+        y[j] = (to_e4m3(x[0], x[1], x[2], x[3]) & mask) | (y[j] & ~mask);
+      }
+      *to = y;
+    }
+    if (tid == 0) v.v_scale[block] = s;
+  }
+}
+
+// Block (layer, b, f, h) of a destination, gathered from the source's rows.
 //
 // With TURNS a workgroup goes on to every frames-th block after its first; without, the launch has one for every
 // block that the table can hold.  (4 and 28 layers of 4 sequences, 1187 of 4259 tokens of 4 heads of 128, the table
@@ -203,11 +348,7 @@ struct TokenMap {
 // are, without: 20 and 109.)
 template <int D, int PAGE, bool TURNS>
 __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void compact_kernel(CompactArgs a) {
-  using B = Block<D, PAGE>;
-  __shared__ uint32_t lds[D * B::kRow];
-  __shared__ float red[4];
-  __shared__ TokenMap<PAGE> map;
-  __shared__ uint64_t s_runs;
+  __shared__ MoveShared<D, PAGE> sh;
   const bool values = blockIdx.y != 0;
   const int tid = threadIdx.x;
   unsigned id = blockIdx.x;
@@ -228,136 +369,85 @@ __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void compact_kernel(Com
     int from = src < 0 ? -1 : page_at(a.c, src, min(r / PAGE, a.c.max_pages - 1));
     const int n = L < a.P + a.K_in || src == dst ? 0 : min(L - a.K_in + a.n_kept, room);
     if (f * PAGE >= n) return;
-    if (page >= 0) {
-      const int hi = min(n - f * PAGE, PAGE), at = r % PAGE;
-      if (tid >= hi) from = -1;
-      const size_t layer_blocks = (size_t)layer * a.c.n_pages * a.c.H_kv;
-      const uint8_t* data = (values ? a.c.v : a.c.k) + (layer_blocks + h) * (PAGE * D);
-      const float* scales = (values ? a.c.v_scale : a.c.k_scale) + layer_blocks + h;
-      if (tid < 64) {
-        if (tid < PAGE) {
-          map.block[tid] = from;
-          reinterpret_cast<uint8_t*>(map.at)[tid] = (uint8_t)at;
-          map.scale[tid] = from >= 0 ? scales[(size_t)from * a.c.H_kv] : 0.f;
-        }
-        const int before = __shfl_up(from, 1, 64);
-        const uint64_t starts = __ballot(tid < hi && (tid == 0 || from != before));
-        if (tid == 0) s_runs = starts;  // tokens whose page is not the one before's
-      }
-      __syncthreads();
-      const size_t block = layer_blocks + (size_t)page * a.c.H_kv + h;
-      if (!values) {
-        float x[B::kPer][4][8], m = 0.f;
-#pragma unroll
-        for (int u = 0; u < B::kPer; ++u) {
-          const int e = tid + u * B::kThreads;
-          const int c = e % (D / 8) * 8, t0 = e / (D / 8) * 4;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int t = t0 + i;
-            const int from = t < hi ? map.block[t] : -1;
-            const int row = reinterpret_cast<const uint8_t*>(map.at)[t];
-            const u32x2 w = from >= 0 ? *reinterpret_cast<const u32x2*>(data + (size_t)from * a.c.H_kv * (PAGE * D) +
-                                                                        row * D + c)
-                                      : u32x2{0u, 0u};
-            float y[2][4];
-            from_e4m3(w[0], y[0]);
-            from_e4m3(w[1], y[1]);
-            const float s = from >= 0 ? map.scale[t] : 0.f;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-              x[u][i][q] = y[q >> 2][q & 3] * s;
-              m = fmaxf(m, fabsf(x[u][i][q]));
-            }
-          }
-        }
-        const float s = block_scale(block_max<B::kThreads>(m, red));
-        store_block<D, PAGE>(a.c.k + block * (PAGE * D), false, 0, hi, pow2_inverse(s), 1.f, x, lds);
-        if (tid == 0) a.c.k_scale[block] = s;
-      } else {
-        // a thread's items: 16 tokens of a channel, as bytes
-        constexpr int kGroups = PAGE / 16, kItems = D * kGroups / B::kThreads;
-        static_assert(kItems * B::kThreads == D * kGroups, "whole items");
-        u32x4 w[kItems], next[kItems], at16[kItems];
-        uint64_t runs = s_runs;
-        auto fetch = [&](int t) {
-          const int from = map.block[t];
-#pragma unroll
-          for (int i = 0; i < kItems; ++i)
-            next[i] = from >= 0 ? ldg16(data + (size_t)from * a.c.H_kv * (PAGE * D) + (tid + i * B::kThreads) * 16)
-                                : zero4();
-        };
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-          w[i] = zero4();
-          at16[i] = map.at[(tid + i * B::kThreads) % kGroups];
-        }
-        int r0 = 0;
-        fetch(0);
-        while (r0 < hi) {
-          runs &= runs - 1;
-          const int r1 = runs ? __builtin_ctzll(runs) : hi;
-#pragma unroll
-          for (int i = 0; i < kItems; ++i) {
-            const int e = tid + i * B::kThreads;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) lds[e / kGroups * B::kRow + e % kGroups * 4 + j] = next[i][j];
-          }
-          __syncthreads();
-          if (r1 < hi) fetch(r1);
-#pragma unroll
-          for (int i = 0; i < kItems; ++i) {
-            const int e = tid + i * B::kThreads, t0 = e % kGroups * 16;
-            const uint8_t* row = reinterpret_cast<const uint8_t*>(lds + e / kGroups * B::kRow);
-            // a byte for every token, those of other blocks dropped: the reads wait for nothing
-            uint32_t byte[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) byte[j] = row[(at16[i][j >> 2] >> (8 * (j & 3))) & 0xff];
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-              w[i][j >> 2] |= t0 + j >= r0 && t0 + j < r1 ? byte[j] << (8 * (j & 3)) : 0u;
-          }
-          __syncthreads();
-          r0 = r1;
-        }
-        float m = 0.f;
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-          const int t0 = (tid + i * B::kThreads) % kGroups * 16;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float y[4];
-            from_e4m3(w[i][j], y);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) m = fmaxf(m, fabsf(y[q]) * map.scale[t0 + 4 * j + q]);
-          }
-        }
-        const float s = block_scale(block_max<B::kThreads>(m, red)), inv = pow2_inverse(s);
-        uint8_t* out = a.c.v + block * (PAGE * D);
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-          const int e = tid + i * B::kThreads, t0 = e % kGroups * 16;
-          if (t0 >= hi) continue;
-          u32x4* to = reinterpret_cast<u32x4*>(out + e * 16);
-          u32x4 y = t0 + 16 > hi ? *to : zero4();  // tokens past the last are kept
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float x[4];
-            from_e4m3(w[i][j], x);
-#pragma unroll
-            // (one factor after the other: a block of zeros has the smallest scale, and the product of the two
-            // passes fp32's range)
-            for (int q = 0; q < 4; ++q) x[q] = x[q] * map.scale[t0 + 4 * j + q] * inv;
-            const int n_t = hi - t0 - 4 * j;  // tokens of this word
-            const uint32_t mask = n_t >= 4 ? ~0u : n_t <= 0 ? 0u : (1u << (8 * n_t)) - 1u;
-            y[j] = (to_e4m3(x[0], x[1], x[2], x[3]) & mask) | (y[j] & ~mask);
-          }
-          *to = y;
-        }
-        if (tid == 0) a.c.v_scale[block] = s;
-      }
-    }
+    if (page >= 0) move_block<D, PAGE>(a.c, layer, h, values, page, from, r % PAGE, min(n - f * PAGE, PAGE), sh);
     if (!TURNS || f + a.frames > (n - 1) / PAGE) return;
+    f += a.frames;
+    __syncthreads();  // the block's LDS is read before the next one's is written
+  }
+}
+
+// Eviction's rows into their new pages: block (layer, b, f, h) of request b as its
+// kept tokens say (evict_select_kernel, evict_pages_kernel); the old pages are in
+// `old`, since the table has the new ones already.  The last B workgroups (of keys)
+// do what no block depends on any more: the old pages' counts, the table's end, the
+// length, and the scores, which move down in place, each round's reads before its writes.
+template <int D, int PAGE>
+__device__ __forceinline__ void evict_finish(const EvictArgs& a, const EvictInfo& e, int b) {
+  constexpr int NT = Block<D, PAGE>::kThreads, kPer = 8;
+  const int tid = threadIdx.x;
+  int32_t* kept = a.kept_idx + (size_t)b * a.n_keep;
+  if (e.slot < 0) {  // (nothing is evicted; the list is cleared already if nothing was to be)
+    if (e.n < e.len)
+      for (int i = tid; i < a.n_keep; i += NT) kept[i] = -1;
+    return;
+  }
+  const int want = (e.n + PAGE - 1) / PAGE, have = (e.len + PAGE - 1) / PAGE;
+  const int32_t* old = a.old + (size_t)b * a.c.max_pages;
+  int32_t* row = const_cast<int32_t*>(a.c.table) + (size_t)e.slot * a.c.max_pages;
+  for (int j = e.first_page + tid; j < have; j += NT) {
+    const int p = old[j];
+    if (p >= 0 && p < a.c.n_pages && atomicSub(&a.ref[p], 1) <= 0) atomicAdd(&a.ref[p], 1);  // never below 0
+    if (j >= want) row[j] = -1;
+  }
+  if (tid == 0) const_cast<int32_t*>(a.c.len)[e.slot] = e.n;
+  float* score = a.score + (size_t)e.slot * a.c.max_pages * PAGE;
+  for (int i0 = e.moved; i0 < e.n; i0 += NT * kPer) {
+    float x[kPer];
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      const int i = i0 + q * NT + tid;
+      x[q] = i < e.n ? score[min(max(kept[i], 0), e.len - 1)] : 0.f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      const int i = i0 + q * NT + tid;
+      if (i < e.n) score[i] = x[q];
+    }
+    __syncthreads();
+  }
+  for (int i = e.n + tid; i < e.len; i += NT) score[i] = 0.f;
+}
+
+template <int D, int PAGE, bool TURNS>
+__global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void evict_kernel(EvictArgs a) {
+  __shared__ MoveShared<D, PAGE> sh;
+  const bool values = blockIdx.y != 0;
+  const int tid = threadIdx.x;
+  unsigned id = blockIdx.x;
+  const unsigned moves = gridDim.x - a.B;
+  if (id >= moves) {
+    if (!values) evict_finish<D, PAGE>(a, a.info[id - moves], id - moves);
+    return;
+  }
+  const int h = (int)(id % a.c.H_kv);
+  id /= a.c.H_kv;
+  int f = (int)(id % a.frames);
+  id /= a.frames;
+  const int b = (int)(id % a.B), layer = (int)(id / a.B);
+  const EvictInfo e = a.info[b];
+  if (e.slot < 0) return;
+  f += e.first_page;
+  const int last = (e.n + PAGE - 1) / PAGE;  // one past the last page that is written (none if nothing moved)
+  const int32_t* old = a.old + (size_t)b * a.c.max_pages;
+  while (e.moved < e.n && f < last) {
+    const int r = a.kept_idx[(size_t)b * a.n_keep + min(f * PAGE + min(tid, PAGE - 1), e.n - 1)];
+    const int at = min(max(r, 0), e.len - 1);
+    const int from = old[at / PAGE], page = page_at(a.c, e.slot, f);
+    if (page >= 0)
+      move_block<D, PAGE>(a.c, layer, h, values, page, from < a.c.n_pages ? from : -1, at % PAGE,
+                          min(e.n - f * PAGE, PAGE), sh);
+    if (!TURNS) return;
     f += a.frames;
     __syncthreads();  // the block's LDS is read before the next one's is written
   }
@@ -418,6 +508,18 @@ hipError_t launch_kv8_compact(const CompactArgs& a, int d_head, int page, hipStr
       hipLaunchKernelGGL((compact_kernel<D, PAGE, true>), grid, block, 0, s, a);
     else
       hipLaunchKernelGGL((compact_kernel<D, PAGE, false>), grid, block, 0, s, a);
+  });
+}
+
+hipError_t launch_kv8_evict(const EvictArgs& a, int d_head, int page, hipStream_t s) {
+  const dim3 grid((unsigned)a.n_layers * a.B * a.frames * a.c.H_kv + a.B, 2);
+  return by_shape(d_head, page, [&](auto d, auto p) {
+    constexpr int D = decltype(d)::value, PAGE = decltype(p)::value;
+    const dim3 block(Block<D, PAGE>::kThreads);
+    if (a.turns)
+      hipLaunchKernelGGL((evict_kernel<D, PAGE, true>), grid, block, 0, s, a);
+    else
+      hipLaunchKernelGGL((evict_kernel<D, PAGE, false>), grid, block, 0, s, a);
   });
 }
 

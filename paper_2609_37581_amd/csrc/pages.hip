@@ -250,7 +250,186 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(PagesArgs a, c
   if (cow) atomicSub(&a.ref[last], 1);
 }
 
+// Pages for what evict_select_kernel chose to keep, from those that are free before
+// the call; a thread to a request.
+__global__ __launch_bounds__(kReserveThreads) void evict_pages_kernel(EvictArgs e, PagesArgs a) {
+  __shared__ int l_slot[kReserveThreads], l_off[kReserveThreads + 1], l_col[kReserveThreads], l_need[kReserveThreads];
+  __shared__ int red[kReserveThreads / 64];
+  __shared__ int l_total;
+  const int i = threadIdx.x;
+  const uint32_t bits0 = free_bits(a, 8 * i);
+  EvictInfo x = {-1, 0, 0, 0, 0};
+  if (i < a.n) x = e.info[i];
+  bool ok = x.slot >= 0;
+  int need = ok && x.moved < x.n ? pages_of(a, x.n) - x.first_page : 0;
+  l_slot[i] = x.slot;
+  l_col[i] = x.first_page;
+  l_need[i] = ok ? need : -1;
+  // all needs, which may pass 32 bits, by halves
+  int low, high;
+  block_excl_scan(need & 0xffff, red, low);
+  block_excl_scan(need >> 16, red, high);
+  const long long sum = ((long long)high << 16) + low;
+  long long n_free = 0;
+  for (long long p0 = 0; p0 < a.n_pages && n_free < sum; p0 += 8 * kReserveThreads) {
+    int total;
+    block_excl_scan(__popc(p0 ? free_bits(a, p0 + 8 * i) : bits0), red, total);
+    n_free += total;
+  }
+  if (sum > n_free) {
+    // a shortage: in order, each request that still fits is served
+    if (i == 0) {
+      int at = 0;
+      for (int j = 0; j < a.n; ++j) {
+        l_off[j] = at;
+        if (l_need[j] < 0) continue;
+        if (l_need[j] > n_free - at)
+          l_need[j] = -1;
+        else
+          at += l_need[j];
+      }
+      l_total = at;
+    }
+    __syncthreads();
+    ok = l_need[i] >= 0;
+    if (i >= a.n) l_off[i] = l_total;
+    if (i == 0) l_off[kReserveThreads] = l_total;
+  } else {
+    int total;
+    l_off[i] = block_excl_scan(need, red, total);
+    if (i == 0) l_off[kReserveThreads] = l_total = total;
+  }
+  __syncthreads();
+  const int total = l_total;
+  const int reach = a.n > 1 ? 1 << (31 - __builtin_clz(a.n - 1)) : 0;  // largest power of two below n
+  int base = 0;
+  for (long long p0 = 0; p0 < a.n_pages && base < total; p0 += 8 * kReserveThreads) {
+    const long long p = p0 + 8 * i;
+    uint32_t bits = p0 ? free_bits(a, p) : bits0;
+    int sum_step;
+    int r = base + block_excl_scan(__popc(bits), red, sum_step);
+    base += sum_step;
+    int at = 0;  // the last request whose range begins at or before r
+    if (bits && r < total)
+      for (int step = reach; step > 0; step >>= 1) at += l_off[at + step] <= r ? step : 0;
+    while (bits && r < total) {
+      while (l_off[at + 1] <= r) ++at;  // (l_off[n] = total)
+      const int k = __builtin_ctz(bits);
+      bits &= bits - 1;
+      a.table[(size_t)l_slot[at] * a.max_pages + l_col[at] + r - l_off[at]] = (int)(p + k);
+      a.ref[p + k] = 1;
+      ++r;
+    }
+  }
+  if (i >= a.n) return;
+  e.n_evicted[i] = ok ? x.len - x.n : 0;
+  if (x.slot >= 0 && !ok) e.info[i].slot = -1;
+}
+
+// A group's entries: the slot of each (-1: the entry does nothing) and the entry
+// whose sequence it takes over (its own: it keeps what it has).
+struct Group {
+  int slot[TREVS_MAX_BEAMS], src[TREVS_MAX_BEAMS], len[TREVS_MAX_BEAMS];
+};
+__device__ __forceinline__ void read_group(const PagesArgs& a, int g, int width, const int32_t* slots,
+                                           const int32_t* parent, Group& s) {
+  const int tid = threadIdx.x;
+  for (int w = tid; w < width; w += blockDim.x) {
+    const int i = g * width + w, slot = request_slot(a, slots, i);
+    s.slot[w] = slot;
+    s.len[w] = slot_len(a.len, slot, a.max_pages << a.page_shift);
+  }
+  __syncthreads();
+  if (slots) {  // an earlier entry's slot
+    const int n = (g + 1) * width;
+    for (int e = tid; e < n * width; e += blockDim.x) {
+      const int w = e / n, j = e - w * n;
+      if (j < g * width + w && slots[j] == slots[g * width + w]) s.slot[w] = -1, s.len[w] = 0;
+    }
+    __syncthreads();
+  }
+  for (int w = tid; w < width; w += blockDim.x) {
+    const int p = parent[g * width + w];
+    s.src[w] = s.slot[w] >= 0 && p >= 0 && p < width && s.slot[p] >= 0 ? p : w;
+  }
+  __syncthreads();
+}
+
+constexpr int kReorderThreads = 128;
+
+// A thread holds a column of the group, so reads are done before writes.
+__global__ __launch_bounds__(kReorderThreads) void reorder_scores_kernel(PagesArgs a, int width, const int32_t* slots,
+                                                                         const int32_t* parent, float* score) {
+  __shared__ Group s;
+  __shared__ float held[TREVS_MAX_BEAMS][kReorderThreads];
+  const int tid = threadIdx.x, g = blockIdx.y;
+  read_group(a, g, width, slots, parent, s);
+  int longest = 0;
+  for (int w = 0; w < width; ++w) longest = max(longest, s.len[w]);
+  const size_t row = (size_t)a.max_pages << a.page_shift;
+  for (int j = blockIdx.x * kReorderThreads + tid; j < longest; j += gridDim.x * kReorderThreads) {
+#pragma unroll 8
+    for (int w = 0; w < width; ++w) held[w][tid] = s.slot[w] >= 0 ? score[s.slot[w] * row + j] : 0.f;
+    for (int w = 0; w < width; ++w) {
+      const int p = s.src[w];
+      if (p != w && j < max(s.len[w], s.len[p])) score[s.slot[w] * row + j] = j < s.len[p] ? held[p][tid] : 0.f;
+    }
+  }
+}
+
+__global__ __launch_bounds__(kReorderThreads) void reorder_kernel(PagesArgs a, int width, const int32_t* slots,
+                                                                  const int32_t* parent) {
+  __shared__ Group s;
+  __shared__ int held[TREVS_MAX_BEAMS][kReorderThreads];
+  const int tid = threadIdx.x, g = blockIdx.x;
+  read_group(a, g, width, slots, parent, s);
+  int longest = 0;
+  for (int w = 0; w < width; ++w) longest = max(longest, s.len[w]);
+  for (int j = tid; j < pages_of(a, longest); j += kReorderThreads) {
+#pragma unroll 8
+    for (int w = 0; w < width; ++w) held[w][tid] = s.slot[w] >= 0 ? a.table[(size_t)s.slot[w] * a.max_pages + j] : -1;
+    for (int w = 0; w < width; ++w) {
+      const int p = s.src[w];
+      if (p == w) continue;
+      const int old = j < pages_of(a, s.len[w]) ? held[w][tid] : -1, now = j < pages_of(a, s.len[p]) ? held[p][tid] : -1;
+      if (j >= pages_of(a, max(s.len[w], s.len[p]))) continue;
+      a.table[(size_t)s.slot[w] * a.max_pages + j] = now;
+      if (old == now) continue;
+      if (now >= 0 && now < a.n_pages) atomicAdd(&a.ref[now], 1);
+      if (old >= 0 && old < a.n_pages && atomicSub(&a.ref[old], 1) <= 0) atomicAdd(&a.ref[old], 1);  // never below 0
+    }
+  }
+  for (int w = tid; w < width; w += kReorderThreads)
+    if (s.src[w] != w) a.len[s.slot[w]] = s.len[s.src[w]];
+}
+
 }  // namespace
+
+hipError_t launch_evict_pages(const EvictArgs& e, hipStream_t s) {
+  PagesArgs a;
+  a.table = const_cast<int32_t*>(e.c.table);
+  a.len = const_cast<int32_t*>(e.c.len);
+  a.ref = e.ref;
+  a.n_pages = e.c.n_pages;
+  a.n_slots = e.c.n_slots;
+  a.max_pages = e.c.max_pages;
+  a.page_shift = e.page_shift;
+  a.n = e.B;
+  hipLaunchKernelGGL(evict_pages_kernel, dim3(1), dim3(kReserveThreads), 0, s, e, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_reorder(const PagesArgs& a, int groups, int width, const int32_t* slots, const int32_t* parent,
+                                float* score, hipStream_t s) {
+  if (score) {
+    const long long tokens = (long long)a.max_pages << a.page_shift;
+    const int blocks = (int)min((tokens + kReorderThreads - 1) / kReorderThreads, 4096LL / groups + 1);
+    hipLaunchKernelGGL(reorder_scores_kernel, dim3(blocks, groups), dim3(kReorderThreads), 0, s, a, width, slots,
+                       parent, score);
+  }
+  hipLaunchKernelGGL(reorder_kernel, dim3(groups), dim3(kReorderThreads), 0, s, a, width, slots, parent);
+  return hipGetLastError();
+}
 
 hipError_t launch_pages_reserve(const PagesArgs& a, const int32_t* slots, const int32_t* n_new, int32_t* granted,
                                 int32_t* copy_src, int32_t* copy_dst, hipStream_t s) {

@@ -34,6 +34,8 @@ SOFTMAX = {"visual": 0, "causal": 1}  # trevs_softmax
 ROPE_SCALING = {"none": 0, "linear": 1, "parts": 2}  # trevs_rope_scaling
 MAX_POS_PLANES = 4
 MAX_PAGE_REQUESTS = 1024
+MAX_BEAMS = 64
+MAX_BEAM_OUT = 64
 
 _STATUS = {0: "ok", 1: "invalid argument", 2: "unsupported", 3: "workspace", 4: "hip error"}
 
@@ -121,6 +123,32 @@ class Kv8CompactArgs(ctypes.Structure):
     _fields_ = [("struct_size", c_uint32), ("B", c_int32), ("P", c_int32), ("K_in", c_int32),
                 ("n_kept", c_int32), ("kept_idx", c_void_p), ("src_slots", c_void_p),
                 ("dst_slots", c_void_p)]
+
+
+class NormRopeArgs(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("eps", c_float), ("weight_offset", c_float),
+                ("weight_dtype", c_int32), ("per_head", c_int32), ("q_weight", c_void_p),
+                ("k_weight", c_void_p), ("rope", RopeArgs)]
+
+
+class Kv8WeightsArgs(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("B", c_int32), ("T_max", c_int32), ("H_q", c_int32),
+                ("layer", c_int32), ("dtype", c_int32), ("causal", c_int32), ("kv_max", c_int32),
+                ("scale", c_float), ("decay", c_float), ("q", c_void_p), ("q_ld", c_int64),
+                ("q_len", c_void_p), ("slots", c_void_p), ("lse", c_void_p), ("score", c_void_p)]
+
+
+class Kv8EvictArgs(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("B", c_int32), ("n_keep", c_int32), ("n_first", c_int32),
+                ("n_last", c_int32), ("keep", c_void_p), ("slots", c_void_p), ("score", c_void_p),
+                ("n_evicted", c_void_p), ("kept_idx", c_void_p)]
+
+
+class BeamSelectArgs(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("B", c_int32), ("W", c_int32), ("V", c_int32),
+                ("n_out", c_int32), ("dtype", c_int32), ("eos", c_int32), ("logits", c_void_p),
+                ("logits_ld", c_int64), ("score", c_void_p), ("done", c_void_p),
+                ("score_out", c_void_p), ("parent", c_void_p), ("token", c_void_p)]
 
 
 def _torch_empty(shape, dtype, device):
@@ -211,12 +239,32 @@ def lib():
         L.trevs_kv8_attention.restype = ctypes.c_int
         L.trevs_kv8_compact.argtypes = [cache, ctypes.POINTER(Kv8CompactArgs), c_void_p]
         L.trevs_kv8_compact.restype = ctypes.c_int
+        L.trevs_norm_rope.argtypes = [ctypes.POINTER(NormRopeArgs), c_void_p]
+        L.trevs_norm_rope.restype = ctypes.c_int
+        L.trevs_kv8_weights_workspace_size.argtypes = [cache, ctypes.POINTER(Kv8WeightsArgs)]
+        L.trevs_kv8_weights_workspace_size.restype = c_size_t
+        L.trevs_kv8_weights.argtypes = [cache, ctypes.POINTER(Kv8WeightsArgs), c_void_p, c_size_t, c_void_p]
+        L.trevs_kv8_weights.restype = ctypes.c_int
+        L.trevs_kv8_evict_workspace_size.argtypes = [cache, ctypes.POINTER(Kv8EvictArgs)]
+        L.trevs_kv8_evict_workspace_size.restype = c_size_t
+        L.trevs_kv8_evict.argtypes = [cache, ctypes.POINTER(Kv8EvictArgs), c_void_p, c_size_t, c_void_p]
+        L.trevs_kv8_evict.restype = ctypes.c_int
+        L.trevs_beam_select_workspace_size.argtypes = [ctypes.POINTER(BeamSelectArgs)]
+        L.trevs_beam_select_workspace_size.restype = c_size_t
+        L.trevs_beam_select.argtypes = [ctypes.POINTER(BeamSelectArgs), c_void_p, c_size_t, c_void_p]
+        L.trevs_beam_select.restype = ctypes.c_int
+        L.trevs_pages_reorder.argtypes = [cache, c_int32, c_int32] + [c_void_p] * 4
+        L.trevs_pages_reorder.restype = ctypes.c_int
         for size, struct in ((L.trevs_prellm_args_size, PrellmArgs), (L.trevs_inllm_args_size, InllmArgs),
                              (L.trevs_sensitivity_args_size, SensitivityArgs),
                              (L.trevs_rope_args_size, RopeArgs), (L.trevs_kv8_cache_size, Kv8CacheArgs),
                              (L.trevs_kv8_write_args_size, Kv8WriteArgs),
                              (L.trevs_kv8_attention_args_size, Kv8AttentionArgs),
-                             (L.trevs_kv8_compact_args_size, Kv8CompactArgs)):
+                             (L.trevs_kv8_compact_args_size, Kv8CompactArgs),
+                             (L.trevs_norm_rope_args_size, NormRopeArgs),
+                             (L.trevs_kv8_weights_args_size, Kv8WeightsArgs),
+                             (L.trevs_kv8_evict_args_size, Kv8EvictArgs),
+                             (L.trevs_beam_select_args_size, BeamSelectArgs)):
             size.restype = c_size_t
             if size() == ctypes.sizeof(struct):
                 continue
@@ -648,6 +696,43 @@ def rope_frequencies(rot_dim, *, base=10000.0, scaling="none", factor=1.0, origi
     return out
 
 
+def _fill_rope(a, q, k, pos, freqs, sections, interleaved, attn_factor, inplace):
+    """The arguments of a rotation (inverse aside) and its outputs."""
+    dev = q.device
+    dt = q.dtype
+    if dev.type != "cuda":
+        raise ValueError("q must be on a GPU")
+    a.struct_size = ctypes.sizeof(RopeArgs)
+    a.dtype = _dtype_code(q)
+    a.q_ld = _row_ld(q, "q", dev, dt)
+    a.B, a.S, a.H_q, a.d_head = q.shape
+    if k is not None:
+        a.k_ld = _row_ld(k, "k", dev, dt)
+        if k.shape[:2] != q.shape[:2] or k.shape[3] != q.shape[3]:
+            raise ValueError("inconsistent shapes of q and k")
+        a.H_k = k.shape[2]
+    _check(pos, "pos", dev, 3, torch.int64)
+    _check(freqs, "freqs", dev, 1, torch.float64)
+    if pos.shape[1:] != q.shape[:2]:
+        raise ValueError("pos must be [n_pos,B,S]")
+    a.rot_dim, a.n_pos = 2 * freqs.shape[0], pos.shape[0]
+    sections = [a.rot_dim // 2] if sections is None else [int(n) for n in sections]
+    if len(sections) > MAX_POS_PLANES or len(sections) != a.n_pos:
+        raise ValueError(f"sections must give the pairs of each of up to {MAX_POS_PLANES} planes")
+    for i, n in enumerate(sections):
+        a.section[i] = n
+    a.interleaved, a.attn_factor = int(interleaved), attn_factor
+    if inplace:
+        q_out, k_out = q, k
+        a.q_out_ld, a.k_out_ld = a.q_ld, a.k_ld
+    else:
+        q_out = _empty(q.shape, dt, dev)
+        k_out = None if k is None else _empty(k.shape, dt, dev)
+    a.freqs, a.pos, a.q, a.k = _ptr(freqs), _ptr(pos), _ptr(q), _ptr(k)
+    a.q_out, a.k_out = _ptr(q_out), _ptr(k_out)
+    return q_out, k_out
+
+
 class Rope:
     """Rotary positions of query rows q [B,S,H_q,d] and, unless None, key rows
     k [B,S,H_k,d] at pos [n_pos,B,S] int64, with freqs [R/2] float64 on the
@@ -659,41 +744,11 @@ class Rope:
 
     def __init__(self, q, k, pos, *, freqs, sections=None, interleaved=False, inverse=False,
                  attn_factor=1.0, inplace=False):
-        self.device = dev = q.device
-        dt = q.dtype
-        if dev.type != "cuda":
-            raise ValueError("q must be on a GPU")
-        a = RopeArgs()
-        a.struct_size = ctypes.sizeof(RopeArgs)
-        a.dtype = _dtype_code(q)
-        a.q_ld = _row_ld(q, "q", dev, dt)
-        a.B, a.S, a.H_q, a.d_head = q.shape
-        if k is not None:
-            a.k_ld = _row_ld(k, "k", dev, dt)
-            if k.shape[:2] != q.shape[:2] or k.shape[3] != q.shape[3]:
-                raise ValueError("inconsistent shapes of q and k")
-            a.H_k = k.shape[2]
-        _check(pos, "pos", dev, 3, torch.int64)
-        _check(freqs, "freqs", dev, 1, torch.float64)
-        if pos.shape[1:] != q.shape[:2]:
-            raise ValueError("pos must be [n_pos,B,S]")
-        a.rot_dim, a.n_pos = 2 * freqs.shape[0], pos.shape[0]
-        sections = [a.rot_dim // 2] if sections is None else [int(n) for n in sections]
-        if len(sections) > MAX_POS_PLANES or len(sections) != a.n_pos:
-            raise ValueError(f"sections must give the pairs of each of up to {MAX_POS_PLANES} planes")
-        for i, n in enumerate(sections):
-            a.section[i] = n
-        a.interleaved, a.inverse, a.attn_factor = int(interleaved), int(inverse), attn_factor
-        if inplace:
-            self.q_out, self.k_out = q, k
-            a.q_out_ld, a.k_out_ld = a.q_ld, a.k_ld
-        else:
-            self.q_out = _empty(q.shape, dt, dev)
-            self.k_out = None if k is None else _empty(k.shape, dt, dev)
-        a.freqs, a.pos, a.q, a.k = _ptr(freqs), _ptr(pos), _ptr(q), _ptr(k)
-        a.q_out, a.k_out = _ptr(self.q_out), _ptr(self.k_out)
+        self.device = q.device
+        self.args = a = RopeArgs()
+        self.q_out, self.k_out = _fill_rope(a, q, k, pos, freqs, sections, interleaved, attn_factor, inplace)
+        a.inverse = int(inverse)
         self.inputs = (q, k, pos, freqs)
-        self.args = a
 
     def __call__(self, stream=None):
         _call(lib().trevs_rope, self.device, stream, ctypes.byref(self.args))
@@ -703,6 +758,44 @@ class Rope:
 def rope(q, k, pos, stream=None, **kw):
     """Rotary positions: returns (q_out, k_out); see Rope."""
     return _one_off(stream, q.device, lambda: Rope(q, k, pos, **kw)(), q, k, pos, kw.get("freqs"))
+
+
+class NormRope:
+    """Rope after an RMS norm of every head: values over the root of their
+    head's mean square (plus eps), times q_weight or k_weight (fp32 or bf16
+    [d_head], or [H,d_head] for a weight a head; None: none) plus
+    weight_offset.  The other arguments are those of Rope."""
+
+    def __init__(self, q, k, pos, *, freqs, q_weight=None, k_weight=None, eps=1e-6, weight_offset=0.0,
+                 sections=None, interleaved=False, attn_factor=1.0, inplace=False):
+        self.device = dev = q.device
+        self.args = a = NormRopeArgs()
+        a.struct_size = ctypes.sizeof(NormRopeArgs)
+        self.q_out, self.k_out = _fill_rope(a.rope, q, k, pos, freqs, sections, interleaved, attn_factor,
+                                            inplace)
+        if k is None and k_weight is not None:
+            raise ValueError("k_weight without k")
+        given = [(w, x, n) for w, x, n in ((q_weight, q, "q_weight"), (k_weight, k, "k_weight"))
+                 if w is not None]
+        for w, x, name in given:
+            _check(w, name, dev, given[0][0].dim(), given[0][0].dtype)
+            if w.shape not in (x.shape[3:], x.shape[2:]):
+                raise ValueError(f"{name} must be [d_head] or [H,d_head]")
+        if given:
+            a.weight_dtype, a.per_head = _dtype_code(given[0][0]), given[0][0].dim() - 1
+        a.eps, a.weight_offset = eps, weight_offset
+        a.q_weight, a.k_weight = _ptr(q_weight), _ptr(k_weight)
+        self.inputs = (q, k, pos, freqs, q_weight, k_weight)
+
+    def __call__(self, stream=None):
+        _call(lib().trevs_norm_rope, self.device, stream, ctypes.byref(self.args))
+        return self.q_out, self.k_out
+
+
+def norm_rope(q, k, pos, stream=None, **kw):
+    """Norms of the heads, then rotary positions: returns (q_out, k_out); see NormRope."""
+    return _one_off(stream, q.device, lambda: NormRope(q, k, pos, **kw)(), q, k, pos, kw.get("freqs"),
+                    kw.get("q_weight"), kw.get("k_weight"))
 
 
 class Kv8Cache:
@@ -948,6 +1041,191 @@ def kv8_compact(cache, kept_idx, src_slots, dst_slots, stream=None, **kw):
     """Kept rows of cached sequences moved together; see Kv8Compact."""
     _one_off(stream, cache.device, lambda: Kv8Compact(cache, kept_idx, src_slots, dst_slots, **kw)(),
              cache, kept_idx, src_slots, dst_slots)
+
+
+def kv8_scores(cache):
+    """Scores of a cache's tokens for Kv8Weights: zeros, float32 [n_slots,
+    max_pages * page_tokens]."""
+    a = cache.args
+    return _empty((a.n_slots, a.max_pages * a.page_tokens), torch.float32, cache.device).zero_()
+
+
+def _check_scores(cache, score):
+    _check(score, "score", cache.device, 2, torch.float32)
+    if score.shape != (cache.args.n_slots, cache.args.max_pages * cache.args.page_tokens):
+        raise ValueError("score must be [n_slots, max_pages * page_tokens] of the cache")
+
+
+class Kv8Weights:
+    """The attention weights that query rows q [B,T,H_q,d] give to the cached
+    tokens of one layer, summed over rows and heads and added to decay * score,
+    in place.  lse [B,H_q,T] is Kv8Attention's for the same q, q_len, slots,
+    layer, causal, scale and kv_max; slots name no slot twice.  decay=0 begins
+    a slot's scores anew.  call() enqueues and returns score."""
+
+    def __init__(self, cache, q, lse, score, q_len=None, slots=None, *, layer=0, causal=True, scale=None,
+                 kv_max=0, decay=1.0):
+        dev, dt = cache.device, q.dtype
+        a = Kv8WeightsArgs()
+        a.struct_size = ctypes.sizeof(Kv8WeightsArgs)
+        a.dtype = _dtype_code(q)
+        a.q_ld = _row_ld(q, "q", dev, dt)
+        if q.shape[3] != cache.args.d_head:
+            raise ValueError("q must be [B,T,H_q,d_head] of the cache")
+        a.B, a.T_max, a.H_q, _ = q.shape
+        _check(lse, "lse", dev, 3, torch.float32)
+        if lse.shape != (a.B, a.H_q, a.T_max):
+            raise ValueError("lse must be [B,H_q,T]")
+        _check_scores(cache, score)
+        _check_list(q_len, "q_len", dev, a.B)
+        _check_list(slots, "slots", dev, a.B)
+        a.layer, a.causal, a.kv_max, a.decay = layer, int(causal), kv_max, decay
+        a.scale = float(scale) if scale is not None else q.shape[3] ** -0.5
+        a.q, a.q_len, a.slots = _ptr(q), _ptr(q_len), _ptr(slots)
+        a.lse, a.score = _ptr(lse), _ptr(score)
+        self.cache, self.inputs, self.args, self.score = cache, (q, lse, q_len, slots), a, score
+        ws = lib().trevs_kv8_weights_workspace_size(ctypes.byref(cache.args), ctypes.byref(a))
+        if ws == 0:
+            st = lib().trevs_kv8_weights(ctypes.byref(cache.args), ctypes.byref(a), None, 0, None)
+            raise TrevsError(st, "trevs_kv8_weights")
+        self.workspace = _empty((ws,), torch.uint8, dev)
+
+    def __call__(self, stream=None):
+        _call(lib().trevs_kv8_weights, self.cache.device, stream, ctypes.byref(self.cache.args),
+              ctypes.byref(self.args), self.workspace.data_ptr(), self.workspace.numel())
+        return self.score
+
+
+def kv8_weights(cache, q, lse, score, q_len=None, slots=None, stream=None, **kw):
+    """Attention weights added to the tokens' scores: returns score; see Kv8Weights."""
+    return _one_off(stream, cache.device, lambda: Kv8Weights(cache, q, lse, score, q_len, slots, **kw)(),
+                    cache, q, lse, score, q_len, slots)
+
+
+class Kv8Evict:
+    """Sequences of slots (None: slots 0..B-1, B given by keep or by `n`; else
+    all) cut to n_keep tokens each, or keep[b] of them: the first n_first, the
+    last n_last, and those of the highest scores between, in their order, in
+    every layer.  Tables, lengths, counts and scores follow.  call() returns
+    (n_evicted [B], kept_idx [B,n_keep]): how many tokens went (0: the sequence
+    is short enough, or the free pages did not suffice), and the places that the
+    kept ones had, -1 past them or where nothing went."""
+
+    def __init__(self, cache, score, slots=None, *, n_keep, n_first=0, n_last=0, keep=None, n=None):
+        dev = cache.device
+        _check_scores(cache, score)
+        a = Kv8EvictArgs()
+        a.struct_size = ctypes.sizeof(Kv8EvictArgs)
+        given = [t.shape[0] for t in (slots, keep) if isinstance(t, torch.Tensor) and t.dim() == 1]
+        a.B = given[0] if given else cache.args.n_slots if n is None else n
+        if n is not None and a.B != n:
+            raise ValueError("n differs from the lists' length")
+        _check_list(slots, "slots", dev, a.B)
+        _check_list(keep, "keep", dev, a.B)
+        a.n_keep, a.n_first, a.n_last = n_keep, n_first, n_last
+        if a.B < 1 or n_keep < 1:
+            raise TrevsError(1, "trevs_kv8_evict")
+        self.n_evicted = _empty((a.B,), torch.int32, dev)
+        self.kept_idx = _empty((a.B, n_keep), torch.int32, dev)
+        a.keep, a.slots, a.score = _ptr(keep), _ptr(slots), _ptr(score)
+        a.n_evicted, a.kept_idx = _ptr(self.n_evicted), _ptr(self.kept_idx)
+        self.cache, self.inputs, self.args = cache, (score, slots, keep), a
+        ws = lib().trevs_kv8_evict_workspace_size(ctypes.byref(cache.args), ctypes.byref(a))
+        if ws == 0:
+            st = lib().trevs_kv8_evict(ctypes.byref(cache.args), ctypes.byref(a), None, 0, None)
+            raise TrevsError(st, "trevs_kv8_evict")
+        self.workspace = _empty((ws,), torch.uint8, dev)
+
+    def __call__(self, stream=None):
+        _call(lib().trevs_kv8_evict, self.cache.device, stream, ctypes.byref(self.cache.args),
+              ctypes.byref(self.args), self.workspace.data_ptr(), self.workspace.numel())
+        return self.n_evicted, self.kept_idx
+
+
+def kv8_evict(cache, score, slots=None, stream=None, **kw):
+    """Sequences cut to their best tokens: returns (n_evicted, kept_idx); see Kv8Evict."""
+    return _one_off(stream, cache.device, lambda: Kv8Evict(cache, score, slots, **kw)(), cache, score, slots,
+                    kw.get("keep"))
+
+
+# --------------------------------------------------------------- beam search
+class BeamSelect:
+    """The n_out best continuations of each sequence over its beams and the
+    vocabulary: logits [B,W,V] (fp32 or bf16; rows evenly spaced), score [B,W]
+    float32, the beams' summed log probabilities; done [B,W] int32 or None:
+    beams that go on by the token eos alone, with their score.  call() returns
+    (score [B,n_out] float32, parent, token [B,n_out] int32), best first, ties
+    to the lower beam and token; (-inf, -1, -1) where there are fewer."""
+
+    def __init__(self, logits, score, done=None, *, n_out, eos=0):
+        if not isinstance(logits, torch.Tensor) or logits.dim() != 3 or min(logits.shape) < 1:
+            raise ValueError("logits must be a non-empty [B,W,V] tensor")
+        self.device = dev = logits.device
+        if dev.type != "cuda":
+            raise ValueError("logits must be on a GPU")
+        B, W, V = logits.shape
+        sb, sw, sv = logits.stride()
+        ld = sw if W > 1 else sb if B > 1 else V
+        if (V > 1 and sv != 1) or (B > 1 and sb != W * ld) or ld < V:
+            raise ValueError("logits must have dense, evenly spaced rows")
+        _check(score, "score", dev, 2, torch.float32)
+        if done is not None:
+            _check(done, "done", dev, 2, torch.int32)
+        if score.shape != (B, W) or (done is not None and done.shape != (B, W)):
+            raise ValueError("score and done must be [B,W]")
+        a = BeamSelectArgs()
+        a.struct_size = ctypes.sizeof(BeamSelectArgs)
+        a.B, a.W, a.V, a.n_out, a.eos = B, W, V, n_out, eos
+        a.dtype, a.logits_ld = _dtype_code(logits), ld
+        if n_out < 1:
+            raise TrevsError(1, "trevs_beam_select")
+        self.score_out = _empty((B, n_out), torch.float32, dev)
+        self.parent, self.token = [_empty((B, n_out), torch.int32, dev) for _ in range(2)]
+        a.logits, a.score, a.done = _ptr(logits), _ptr(score), _ptr(done)
+        a.score_out, a.parent, a.token = _ptr(self.score_out), _ptr(self.parent), _ptr(self.token)
+        self.inputs, self.args = (logits, score, done), a
+        ws = lib().trevs_beam_select_workspace_size(ctypes.byref(a))
+        if ws == 0:
+            raise TrevsError(lib().trevs_beam_select(ctypes.byref(a), None, 0, None), "trevs_beam_select")
+        self.workspace = _empty((ws,), torch.uint8, dev)
+
+    def __call__(self, stream=None):
+        _call(lib().trevs_beam_select, self.device, stream, ctypes.byref(self.args),
+              self.workspace.data_ptr(), self.workspace.numel())
+        return self.score_out, self.parent, self.token
+
+
+def beam_select(logits, score, done=None, stream=None, **kw):
+    """Beam search's selection: returns (score, parent, token); see BeamSelect."""
+    return _one_off(stream, logits.device, lambda: BeamSelect(logits, score, done, **kw)(), logits, score,
+                    done)
+
+
+class PagesReorder:
+    """The beams' sequences after a selection: slots[g * W + w] (int32, None:
+    slot g * W + w) takes over the pages and length that the slot of beam
+    parent[g, w] of its group had before, for all of parent [n_groups,W] int32
+    at once; with score (Kv8Weights'), the scores too.  No page is copied:
+    PagesReserve and Kv8Copy give beams that share a last page their own."""
+
+    def __init__(self, cache, parent, slots=None, *, score=None):
+        dev = cache.device
+        _check(parent, "parent", dev, 2, torch.int32)
+        _check_list(slots, "slots", dev, parent.numel())
+        if score is not None:
+            _check_scores(cache, score)
+        self.cache, self.inputs = cache, (parent, slots, score)
+
+    def __call__(self, stream=None):
+        parent, slots, score = self.inputs
+        _call(lib().trevs_pages_reorder, self.cache.device, stream, ctypes.byref(self.cache.args),
+              parent.shape[0], parent.shape[1], _ptr(slots), _ptr(parent), _ptr(score))
+
+
+def pages_reorder(cache, parent, slots=None, stream=None, **kw):
+    """Sequences taken over from the beams' parents; see PagesReorder."""
+    _one_off(stream, cache.device, lambda: PagesReorder(cache, parent, slots, **kw)(), cache, parent, slots,
+             kw.get("score"))
 
 
 # ---------------------------------------------------------------- HIP events
