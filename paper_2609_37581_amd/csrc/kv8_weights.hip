@@ -31,43 +31,73 @@ __device__ __forceinline__ Span2 sequence(const WeightsArgs& a, int b) {
 // -lse in base 2; -inf, whose weights are 0, for a row that sees nothing.
 __device__ __forceinline__ float row_base(float lse) { return lse == -INFINITY ? -INFINITY : -lse * kLog2e; }
 
-// A wave's 64 keys of KV head h from token j0 on: lane column c holds keys j0 + c and j0 + 32 + c, half of the
-// channels each (16 in turn with the other half).  f is their scale, times the logits'; absent keys have `there` 0.
-template <int D>
-struct Keys {
-  u32x4 w[2][D / 32];
-  float f[2];
+// 8 values of a row as they lie, and their parts.
+template <class E>
+struct Raw {
+  u32x4 w[E::kBytes / 2];
+  __device__ __forceinline__ void load(const void* q, size_t i) {
+    const u32x4* p = reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(q) + i * E::kBytes);
+#pragma unroll
+    for (int j = 0; j < E::kBytes / 2; ++j) w[j] = ldg16(p + j);
+  }
+  __device__ __forceinline__ void parts(u32x4 (&out)[kParts<E>]) const {
+    if constexpr (E::kBytes == 2) {
+      out[0] = w[0];
+    } else {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j >> 2][j & 3]);
+      bf16x8 y[kParts<E>];
+      split_parts<kParts<E>>(x, y);
+#pragma unroll
+      for (int p = 0; p < kParts<E>; ++p) out[p] = __builtin_bit_cast(u32x4, y[p]);
+    }
+  }
+};
+
+// Where a wave's 64 keys lie, of every KV head: lane column c holds keys j0 + c and j0 + 32 + c, half of the
+// channels each (16 in turn with the other half).
+struct Places {
+  size_t block[2];  // page, counted in KV heads' blocks
+  int row[2];       // in the page
   bool there[2];
-  __device__ __forceinline__ void load(const WeightsArgs& a, const Span2& s, int hk, int j0) {
-    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  __device__ __forceinline__ Places(const WeightsArgs& a, const Span2& s, int j0) {
+    const int col = threadIdx.x & 31;
     const int32_t* table = a.c.table + (size_t)max(s.slot, 0) * a.c.max_pages;
     int page[2];
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
       const int j = min(j0 + 32 * y + col, max(s.L - 1, 0));
-      const int p = table[j >> a.page_shift];
-      there[y] = p >= 0 && p < a.c.n_pages;
-      page[y] = there[y] ? p : 0;
+      page[y] = table[j >> a.page_shift];
+      row[y] = j & ((1 << a.page_shift) - 1);
     }
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      const int j = min(j0 + 32 * y + col, max(s.L - 1, 0));
-      const size_t block = (size_t)page[y] * a.c.H_kv + hk;
-      const uint8_t* k = a.c.k + ((block << a.page_shift) + (j & ((1 << a.page_shift) - 1))) * D + 16 * half;
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) w[y][c] = ldg16(k + 32 * c);
-      f[y] = a.c.k_scale[block] * a.scale_log2e;
+      there[y] = page[y] >= 0 && page[y] < a.c.n_pages;
+      block[y] = (size_t)(there[y] ? page[y] : 0) * a.c.H_kv;
     }
   }
 };
+// Channels [C0, C0 + C) of them in KV head hk, 16 bytes a vector.
+template <int D, int C>
+__device__ __forceinline__ void load_keys(const WeightsArgs& a, const Places& at, int hk, int c0, u32x4 (&w)[2][C / 32]) {
+  const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    const uint8_t* k = a.c.k + (((at.block[y] + hk) << a.page_shift) + at.row[y]) * D + c0 + 16 * half;
+#pragma unroll
+    for (int c = 0; c < C / 32; ++c) w[y][c] = ldg16(k + 32 * c);
+  }
+}
 
 // ------------------------------------------------------------------ few rows
 // A workgroup takes 64 tokens of a sequence, its waves the KV heads in turn; up to 32
 // rows a group, whose operand each lane loads for itself.  Bound by the keys' bytes.
-template <class E, int D>
-__global__ __launch_bounds__(64 * kMaxWaves) void few_rows_kernel(WeightsArgs a) {
+template <class E, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(WeightsArgs a) {
   constexpr int NP = kParts<E>;
-  __shared__ float sums[kMaxWaves][kKeys];
+  constexpr int C = E::kBytes == 2 && D >= 128 ? 128 : 64;  // channels whose loads go out together
+  __shared__ float sums[WAVES][kKeys];
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), n_waves = blockDim.x >> 6;
   const int b = blockIdx.x / a.key_blocks, kb = blockIdx.x - b * a.key_blocks;
@@ -77,51 +107,74 @@ __global__ __launch_bounds__(64 * kMaxWaves) void few_rows_kernel(WeightsArgs a)
   float* score = a.score + (size_t)s.slot * a.width;
   if (j0 < s.L) {
     float acc[2] = {0.f, 0.f};
-    const int t = col / a.G, g = col - t * a.G;
+    const Places at(a, s, j0);
+    // (a lane past the last row has the first one's: its weights come to nothing)
     const bool live = col < n_rows;
+    const int t = live ? col / a.G : 0, g = live ? col - t * a.G : 0;
     const int lim = a.causal ? s.L - s.rows + t + 1 : s.L;
     // (rows see more and more keys: the first one's limit is the least)
     const bool whole = !a.causal || s.L - s.rows + 1 >= min(j0 + kKeys, s.L);
     for (int hk = wave; hk < a.c.H_kv && n_rows > 0; hk += n_waves) {
-      Keys<D> k;
-      k.load(a, s, hk, j0);
       const int h = hk * a.G + g;
-      const float nl = live ? row_base(a.lse[((size_t)b * a.H_q + h) * a.T_max + t]) : -INFINITY;
-      const size_t at = ((size_t)b * a.T_max + t) * a.q_ld + (size_t)h * D + 16 * half;
+      const size_t q0 = ((size_t)b * a.T_max + t) * a.q_ld + (size_t)h * D + 16 * half;
+      const float lse = a.lse[((size_t)b * a.H_q + h) * a.T_max + t];
+      float f[2];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) f[y] = a.c.k_scale[at.block[y] + hk] * a.scale_log2e;
       f32x16 x[2];
 #pragma unroll
       for (int y = 0; y < 2; ++y)
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[y][i] = 0.f;
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) {
-        float q[8] = {};
-        if (live) load_row8(a.q, at + c / 2 * 32 + 8 * (c & 1), q, E());
-        bf16x8 qp[NP];
-        split_parts<NP>(q, qp);
+      for (int c0 = 0; c0 < D; c0 += C) {
+        u32x4 w[2][C / 32];
+        Raw<E> q[C / 16];
+        load_keys<D, C>(a, at, hk, c0, w);
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const u32x4 w = k.w[y][c / 2];
-          const bf16x8 kk = c & 1 ? widen(w[2], w[3], 1.f) : widen(w[0], w[1], 1.f);
+        for (int c = 0; c < C / 16; ++c) q[c].load(a.q, q0 + c0 + c / 2 * 32 + 8 * (c & 1));
 #pragma unroll
-          for (int p = NP - 1; p >= 0; --p) x[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qp[p], kk, x[y], 0, 0, 0);
+        for (int c = 0; c < C / 16; ++c) {
+          u32x4 qp[NP];
+          q[c].parts(qp);
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const u32x4 v = w[y][c / 2];
+            const bf16x8 kk = c & 1 ? widen(v[2], v[3], 1.f) : widen(v[0], v[1], 1.f);
+#pragma unroll
+            for (int p = NP - 1; p >= 0; --p)
+              x[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, qp[p]), kk, x[y], 0, 0, 0);
+          }
         }
       }
+      const float nl = live ? row_base(lse) : -INFINITY;
       float sum[2] = {0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if (8 * (i >> 2) >= n_rows) break;
-        const int row = mfma_row(i, half);
-        const float base = __shfl(nl, row, 64);
-        const int n = __shfl(lim, row, 64);
+      for (int i4 = 0; i4 < 4; ++i4) {  // rows 8 i4 .. +7
+        if (8 * i4 < n_rows) {
+          float base[4];
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const float e = __builtin_amdgcn_exp2f(fmaf(x[y][i], k.f[y], base));
-          sum[y] += whole || j0 + 32 * y + col < n ? e : 0.f;
+          for (int q = 0; q < 4; ++q) base[q] = __shfl(nl, mfma_row(4 * i4 + q, half), 64);
+          if (whole) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) sum[y] += __builtin_amdgcn_exp2f(fmaf(x[y][4 * i4 + q], f[y], base[q]));
+          } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int n = __shfl(lim, mfma_row(4 * i4 + q, half), 64);
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(x[y][4 * i4 + q], f[y], base[q]));
+                sum[y] += j0 + 32 * y + col < n ? e : 0.f;
+              }
+            }
+          }
         }
       }
 #pragma unroll
-      for (int y = 0; y < 2; ++y) acc[y] += k.there[y] ? sum[y] : 0.f;
+      for (int y = 0; y < 2; ++y) acc[y] += at.there[y] ? sum[y] : 0.f;
     }
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
@@ -156,17 +209,47 @@ __device__ __forceinline__ int query_swizzle(int row) {
   return D == 64 ? (row >> 1) & 7 : row & 15;
 }
 
+// Rows staged at once: two products' for bf16 rows of up to 128 channels.
+template <class E, int D>
+constexpr int kStage = E::kBytes == 2 && D <= 128 ? 2 * kRows : kRows;
+
 template <class E, int D>
 struct QueryShared {
-  static constexpr int kVecs = kRows * D / 8;  // 8 values each
+  static constexpr int kVecs = kStage<E, D> * D / 8;  // 8 values each
   u32x4 q[2][kParts<E>][kVecs];
-  float4 base[2][kRows / 4];
-  int4 lim[2][kRows / 4];
+  float4 base[2][kStage<E, D> / 4];
+  int4 lim[2][kStage<E, D> / 4];
 };
+
+// The weights of a product's rows for a lane's two keys, summed.  MASKED: a row sees the tokens below its limit.
+template <bool MASKED>
+__device__ __forceinline__ void add_weights(const f32x16 (&x)[2], const float (&f)[2], int j, const float4* base,
+                                            const int4* lim, float (&sum)[2]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 n = base[2 * i];
+    const float nn[4] = {n.x, n.y, n.z, n.w};
+    int ll[4];
+    if constexpr (MASKED) {
+      const int4 l = lim[2 * i];
+      ll[0] = l.x, ll[1] = l.y, ll[2] = l.z, ll[3] = l.w;
+    }
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(x[y][4 * i + q], f[y], nn[q]));
+        if constexpr (MASKED)
+          sum[y] += j + 32 * y < ll[q] ? e : 0.f;
+        else
+          sum[y] += e;
+      }
+  }
+}
 
 template <class E, int D>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void many_rows_kernel(WeightsArgs a) {
-  constexpr int NP = kParts<E>, kVecs = QueryShared<E, D>::kVecs / 256;
+  constexpr int NP = kParts<E>, S = kStage<E, D>, kVecs = QueryShared<E, D>::kVecs / 256;
   __shared__ QueryShared<E, D> sh;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -180,44 +263,44 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void many_rows_kernel(Weight
   const int j0 = kb * 4 * kKeys, jw = j0 + wave * kKeys;
   if (s.slot < 0 || j0 >= s.L) return;
   const int n_rows = s.rows * a.G;
-  // row tiles of which some row sees a key of this workgroup, and this piece of them
+  // stages of which some row sees a key of this workgroup, and this piece of them
   const int t_first = a.causal ? max(j0 - (s.L - s.rows), 0) : 0;
-  const int tile0 = t_first * a.G / kRows, n_tiles = max((n_rows + kRows - 1) / kRows - tile0, 0);
-  const int first = tile0 + (int)((long long)piece * n_tiles / a.pieces);
-  const int end = tile0 + (int)((long long)(piece + 1) * n_tiles / a.pieces);
+  const int stage0 = t_first * a.G / S, n_stages = max((n_rows + S - 1) / S - stage0, 0);
+  const int first = stage0 + (int)((long long)piece * n_stages / a.pieces);
+  const int end = stage0 + (int)((long long)(piece + 1) * n_stages / a.pieces);
   float acc[2] = {0.f, 0.f};
+  const Places at_keys(a, s, jw);
   for (int hk = hg * a.heads; hk < min((hg + 1) * a.heads, a.c.H_kv); ++hk) {
     if (first >= end) break;
-    bf16x8 kk[2][D / 16];
-    float f[2];
-    bool there[2];
-    {
-      Keys<D> k;
-      k.load(a, s, hk, jw);
+    // A thread stages the same 8 channels of every S-th row: it follows its rows' places.  (Dividing each
+    // row's number by G takes as long as the exponentials.)
+    Raw<E> raw[kVecs];
+    const size_t head = ((size_t)b * a.T_max) * a.q_ld + (size_t)hk * a.G * D;
+    const long long step = (long long)(S / a.G) * a.q_ld + S % a.G * D, wrap = a.q_ld - (long long)a.G * D;
+    size_t at[kVecs];
+    int g[kVecs], row = first * S + tid / (D / 8);  // (of vector 0; the others' lie 256 / (D / 8) rows on)
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          kk[y][2 * c] = widen(k.w[y][c][0], k.w[y][c][1], 1.f);
-          kk[y][2 * c + 1] = widen(k.w[y][c][2], k.w[y][c][3], 1.f);
-        }
-        f[y] = k.f[y];
-        there[y] = k.there[y];
-      }
+    for (int i = 0; i < kVecs; ++i) {
+      const int r = row + i * (256 * 8 / D), t = r / a.G;
+      g[i] = r - t * a.G;
+      at[i] = head + (size_t)t * a.q_ld + g[i] * D + tid % (D / 8) * 8;
     }
-    float q[kVecs][8], base = 0.f;
+    float base = 0.f;
     int lim = 0;
-    auto load = [&](int tile) {
+    auto load = [&](int stage) {
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) {
-        const int e = tid + 256 * i, r = tile * kRows + e / (D / 8), t = r / a.G, g = r - t * a.G;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[i][j] = 0.f;
-        if (r < n_rows)
-          load_row8(a.q, ((size_t)b * a.T_max + t) * a.q_ld + (size_t)(hk * a.G + g) * D + e % (D / 8) * 8, q[i], E());
+        // (a row past the last is the first one: its weights come to nothing, but it may hold anything)
+        raw[i].load(a.q, row + i * (256 * 8 / D) < n_rows ? at[i] : head + tid % (D / 8) * 8);
+        at[i] += step;
+        g[i] += S % a.G;
+        const bool over = g[i] >= a.G;
+        at[i] += over ? wrap : 0;
+        g[i] -= over ? a.G : 0;
       }
-      if (tid < kRows) {
-        const int r = tile * kRows + tid, t = r / a.G, h = hk * a.G + r - t * a.G;
+      row += S;
+      if (tid < S) {
+        const int r = stage * S + tid, t = r / a.G, h = hk * a.G + r - t * a.G;
         base = r < n_rows ? row_base(a.lse[((size_t)b * a.H_q + h) * a.T_max + t]) : -INFINITY;
         lim = r >= n_rows ? 0 : a.causal ? s.L - s.rows + t + 1 : s.L;
       }
@@ -226,82 +309,82 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void many_rows_kernel(Weight
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) {
         const int e = tid + 256 * i, r = e / (D / 8), c = e % (D / 8);
-        bf16x8 parts[NP];
-        split_parts<NP>(q[i], parts);
+        u32x4 parts[NP];
+        raw[i].parts(parts);
 #pragma unroll
-        for (int p = 0; p < NP; ++p)
-          sh.q[buf][p][r * (D / 8) + (c ^ query_swizzle<D>(r))] = __builtin_bit_cast(u32x4, parts[p]);
+        for (int p = 0; p < NP; ++p) sh.q[buf][p][r * (D / 8) + (c ^ query_swizzle<D>(r))] = parts[p];
       }
-      if (tid < kRows) {
+      if (tid < S) {
         reinterpret_cast<float*>(sh.base[buf])[tid] = base;
         reinterpret_cast<int*>(sh.lim[buf])[tid] = lim;
       }
     };
-    __syncthreads();  // (the head before has read its last tile)
     load(first);
-    store(0);
+    bf16x8 kk[2][D / 16];
+    float f[2], sum[2] = {0.f, 0.f};
+    {
+      u32x4 w[2][D / 32];
+      load_keys<D, D>(a, at_keys, hk, 0, w);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          kk[y][2 * c] = widen(w[y][c][0], w[y][c][1], 1.f);
+          kk[y][2 * c + 1] = widen(w[y][c][2], w[y][c][3], 1.f);
+        }
+        f[y] = a.c.k_scale[at_keys.block[y] + hk] * a.scale_log2e;
+      }
+    }
+    store(0);  // (the head before ended with a barrier behind its last reads)
     __syncthreads();
-    for (int tile = first; tile < end; ++tile) {
-      const int buf = (tile - first) & 1;
-      load(min(tile + 1, end - 1));
-      // rows see more and more keys: the tile's first and last rows' limits
-      const int least = a.causal ? s.L - s.rows + tile * kRows / a.G + 1 : s.L;
-      const int most = a.causal ? s.L - s.rows + min(tile * kRows + kRows - 1, n_rows - 1) / a.G + 1 : s.L;
+    for (int stage = first; stage < end; ++stage) {
+      const int buf = (stage - first) & 1;
+      if (stage + 1 < end) load(stage + 1);
+      // rows see more and more keys: the limits of the stage's first and last one
+      const int least = a.causal ? s.L - s.rows + stage * S / a.G + 1 : s.L;
+      const int most = a.causal ? s.L - s.rows + min(stage * S + S - 1, n_rows - 1) / a.G + 1 : s.L;
       if (jw < most) {
-        f32x16 x[2];
+        f32x16 x[S / kRows][2];
+        auto product = [&](int u) {
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+          for (int y = 0; y < 2; ++y)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) x[y][i] = 0.f;
+            for (int i = 0; i < 16; ++i) x[u][y][i] = 0.f;
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c)
+          for (int c = 0; c < D / 16; ++c)
 #pragma unroll
-          for (int p = NP - 1; p >= 0; --p) {
-            const int chunk = c / 2 * 4 + 2 * half + (c & 1);
-            const bf16x8 qq =
-                __builtin_bit_cast(bf16x8, sh.q[buf][p][col * (D / 8) + (chunk ^ query_swizzle<D>(col))]);
+            for (int p = NP - 1; p >= 0; --p) {
+              const int chunk = c / 2 * 4 + 2 * half + (c & 1), r = u * kRows + col;
+              const bf16x8 qq =
+                  __builtin_bit_cast(bf16x8, sh.q[buf][p][r * (D / 8) + (chunk ^ query_swizzle<D>(r))]);
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
-              x[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qq, kk[y][c], x[y], 0, 0, 0);
-          }
-        float sum[2] = {0.f, 0.f};
+              for (int y = 0; y < 2; ++y)
+                x[u][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qq, kk[y][c], x[u][y], 0, 0, 0);
+            }
+        };
+        const float4* bases = sh.base[buf] + half;
+        const int4* lims = sh.lim[buf] + half;
+        float part[2] = {0.f, 0.f};
         if (least >= min(jw + kKeys, s.L)) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 n = sh.base[buf][2 * i + half];
+          for (int u = 0; u < S / kRows; ++u) product(u);
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              sum[y] += __builtin_amdgcn_exp2f(fmaf(x[y][4 * i], f[y], n.x));
-              sum[y] += __builtin_amdgcn_exp2f(fmaf(x[y][4 * i + 1], f[y], n.y));
-              sum[y] += __builtin_amdgcn_exp2f(fmaf(x[y][4 * i + 2], f[y], n.z));
-              sum[y] += __builtin_amdgcn_exp2f(fmaf(x[y][4 * i + 3], f[y], n.w));
-            }
-          }
+          for (int u = 0; u < S / kRows; ++u) add_weights<false>(x[u], f, 0, bases + u * (kRows / 4), lims, part);
         } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 n = sh.base[buf][2 * i + half];
-            const int4 l = sh.lim[buf][2 * i + half];
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              const int j = jw + 32 * y + col;
-              const float e0 = __builtin_amdgcn_exp2f(fmaf(x[y][4 * i], f[y], n.x));
-              const float e1 = __builtin_amdgcn_exp2f(fmaf(x[y][4 * i + 1], f[y], n.y));
-              const float e2 = __builtin_amdgcn_exp2f(fmaf(x[y][4 * i + 2], f[y], n.z));
-              const float e3 = __builtin_amdgcn_exp2f(fmaf(x[y][4 * i + 3], f[y], n.w));
-              sum[y] += j < l.x ? e0 : 0.f;
-              sum[y] += j < l.y ? e1 : 0.f;
-              sum[y] += j < l.z ? e2 : 0.f;
-              sum[y] += j < l.w ? e3 : 0.f;
-            }
+          for (int u = 0; u < S / kRows; ++u) {
+            product(u);
+            add_weights<true>(x[u], f, jw + col, bases + u * (kRows / 4), lims + u * (kRows / 4), part);
           }
         }
-#pragma unroll
-        for (int y = 0; y < 2; ++y) acc[y] += there[y] ? sum[y] : 0.f;
+        sum[0] += part[0];
+        sum[1] += part[1];
       }
-      store(buf ^ 1);
+      if (stage + 1 < end) store(buf ^ 1);
       __syncthreads();
     }
+#pragma unroll
+    for (int y = 0; y < 2; ++y) acc[y] += at_keys.there[y] ? sum[y] : 0.f;
   }
 #pragma unroll
   for (int y = 0; y < 2; ++y) {
@@ -335,8 +418,11 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(WeightsArgs a) {
 template <class E, int D>
 hipError_t launch(const WeightsArgs& a, const WeightsPlan& p, hipStream_t s) {
   if (p.few) {
-    hipLaunchKernelGGL((few_rows_kernel<E, D>), dim3((unsigned)(a.B * (long long)a.key_blocks)),
-                       dim3(64 * std::min(a.c.H_kv, kMaxWaves)), 0, s, a);
+    const dim3 grid((unsigned)(a.B * (long long)a.key_blocks)), block(64 * std::min(a.c.H_kv, kMaxWaves));
+    if (a.c.H_kv <= 4)
+      hipLaunchKernelGGL((few_rows_kernel<E, D, 4>), grid, block, 0, s, a);
+    else
+      hipLaunchKernelGGL((few_rows_kernel<E, D, kMaxWaves>), grid, block, 0, s, a);
     return hipGetLastError();
   }
   hipLaunchKernelGGL((many_rows_kernel<E, D>),
