@@ -206,6 +206,7 @@ hipError_t launch_kv8_attention(const AttnArgs& a, const AttnPlan& p, int dtype,
 // into parts of (KV heads, pieces of the rows), summed by a second one.
 struct WeightsPlan {
   bool few;
+  int tokens;               // of a workgroup's block
   int key_blocks, heads, head_groups, pieces;
 };
 struct WeightsArgs {
@@ -221,7 +222,7 @@ struct WeightsArgs {
   float scale_log2e, decay;
   int key_blocks, heads, head_groups, pieces;
 };
-WeightsPlan weights_plan(int B, int T_max, int H_kv, int G, int kv_max);
+WeightsPlan weights_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtype);
 hipError_t launch_kv8_weights(const WeightsArgs& a, const WeightsPlan& p, int dtype, int d_head, hipStream_t s);
 
 struct PagesArgs {

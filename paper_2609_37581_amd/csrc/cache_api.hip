@@ -305,7 +305,7 @@ int weights_keys(const trevs_kv8_cache* c, const trevs_kv8_weights_args* a) {
   return a->kv_max ? a->kv_max : c->max_pages * c->page_tokens;
 }
 WeightsPlan plan_of(const trevs_kv8_cache* c, const trevs_kv8_weights_args* a) {
-  return weights_plan(a->B, a->T_max, c->H_kv, a->H_q / c->H_kv, weights_keys(c, a));
+  return weights_plan(a->B, a->T_max, c->H_kv, a->H_q / c->H_kv, weights_keys(c, a), a->dtype);
 }
 
 trevs_status validate_weights(const trevs_kv8_cache* c, const trevs_kv8_weights_args* a) {
@@ -331,7 +331,7 @@ trevs_status validate_weights(const trevs_kv8_cache* c, const trevs_kv8_weights_
   if (any_overlap(&score, 1, in, 4) || meets_cache(c, score)) return TREVS_ERR_INVALID_ARG;
   const WeightsPlan p = plan_of(c, a);
   const int64_t groups = (int64_t)a->B * p.head_groups * p.key_blocks;
-  if (p.few ? (int64_t)a->B * p.key_blocks > kMaxGroups / 4 : groups > kMaxGroups / p.pieces) return TREVS_ERR_UNSUPPORTED;
+  if (p.few ? (int64_t)a->B * p.key_blocks > INT32_MAX : groups > kMaxGroups / p.pieces) return TREVS_ERR_UNSUPPORTED;
   return TREVS_OK;
 }
 size_t weights_bytes(const trevs_kv8_cache* c, const trevs_kv8_weights_args* a) {

@@ -8,14 +8,16 @@
 // query rows is a sum of its registers, and a key's sum stays in one register
 // however many rows pass by.  Nothing is added by atomics: the order of every sum
 // follows from the sizes.
+#include <type_traits>
+
 #include "rows.hpp"
+#include "cut.hpp"
 
 namespace trevs {
 namespace {
 
 constexpr int kKeys = 64;   // keys of a wave: two columns of 32 a lane
 constexpr int kRows = 32;   // query rows of a product
-constexpr int kMaxWaves = 16;
 
 struct Span2 {
   int slot, rows, L;
@@ -91,113 +93,251 @@ __device__ __forceinline__ void load_keys(const WeightsArgs& a, const Places& at
 }
 
 // ------------------------------------------------------------------ few rows
-// A workgroup takes 64 tokens of a sequence, its waves the KV heads in turn; up to 32
-// rows a group, whose operand each lane loads for itself.  Bound by the keys' bytes.
-template <class E, int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(WeightsArgs a) {
-  constexpr int NP = kParts<E>;
-  constexpr int C = E::kBytes == 2 && D >= 128 ? 128 : 64;  // channels whose loads go out together
-  __shared__ float sums[WAVES][kKeys];
-  const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), n_waves = blockDim.x >> 6;
-  const int b = blockIdx.x / a.key_blocks, kb = blockIdx.x - b * a.key_blocks;
-  const Span2 s = sequence(a, b);
-  if (s.slot < 0) return;
-  const int n_rows = s.rows * a.G, j0 = kb * kKeys;
-  float* score = a.score + (size_t)s.slot * a.width;
-  if (j0 < s.L) {
-    float acc[2] = {0.f, 0.f};
-    const Places at(a, s, j0);
-    // (a lane past the last row has the first one's: its weights come to nothing)
-    const bool live = col < n_rows;
-    const int t = live ? col / a.G : 0, g = live ? col - t * a.G : 0;
-    const int lim = a.causal ? s.L - s.rows + t + 1 : s.L;
-    // (rows see more and more keys: the first one's limit is the least)
-    const bool whole = !a.causal || s.L - s.rows + 1 >= min(j0 + kKeys, s.L);
-    for (int hk = wave; hk < a.c.H_kv && n_rows > 0; hk += n_waves) {
-      const int h = hk * a.G + g;
-      const size_t q0 = ((size_t)b * a.T_max + t) * a.q_ld + (size_t)h * D + 16 * half;
+// Products of 16 x 16: a load takes 64 bytes of each of 16 keys.  A workgroup takes
+// tokens of one sequence, its waves the KV heads in turn, the group's rows in NQ tiles
+// of 16.  Bound by the keys' bytes: a wave's rows stay in its registers over the blocks
+// of a sequence, pages are looked up two blocks ahead and keys loaded one, where there
+// are registers for two (one token of 64 sequences of 1.2 k to 16.5 k tokens, 28/4
+// heads of 128: 62 us, 4.7 TB/s; with the keys of one block 66, streamed past the
+// caches 68, as products of 32 x 32, 32 bytes of each of 32 keys, 83).
+constexpr int kRun = 8;  // blocks whose sums are joined at once
+
+// The calling wave's part of the sums of `run` blocks of 16 Y tokens from j0 on.
+template <class E, int D, int Y, int NQ>
+struct FewRows {
+  Raw<E> q[NQ][D / 32];
+  float nl[NQ];  // of row 16 m + lane % 16
+  int lim[NQ];
+  __device__ __forceinline__ void load(const WeightsArgs& a, const Span2& s, int b, int hk) {
+    const int n16 = threadIdx.x & 15, g4 = (threadIdx.x & 63) >> 4, n_rows = s.rows * a.G;
+#pragma unroll
+    for (int m = 0; m < NQ; ++m) {
+      // (a lane past the last row has the first one's: its weights come to nothing)
+      const int r = 16 * m + n16;
+      const bool live = r < n_rows;
+      const int t = live ? r / a.G : 0, h = hk * a.G + (live ? r - t * a.G : 0);
+      const size_t at = ((size_t)b * a.T_max + t) * a.q_ld + (size_t)h * D + 16 * g4;
       const float lse = a.lse[((size_t)b * a.H_q + h) * a.T_max + t];
-      float f[2];
 #pragma unroll
-      for (int y = 0; y < 2; ++y) f[y] = a.c.k_scale[at.block[y] + hk] * a.scale_log2e;
-      f32x16 x[2];
+      for (int c = 0; c < D / 32; ++c) q[m][c].load(a.q, at + c / 2 * 64 + 8 * (c & 1));
+      nl[m] = live ? lse : -INFINITY;
+      lim[m] = a.causal ? s.L - s.rows + t + 1 : s.L;
+    }
+  }
+  __device__ __forceinline__ void add(const WeightsArgs& a, const Span2& s, int hk, int j0, int run, bool first,
+                                      float* sums) {
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    constexpr int NP = kParts<E>;
+    const int n16 = threadIdx.x & 15, g4 = (threadIdx.x & 63) >> 4;
+    const int32_t* table = a.c.table + (size_t)s.slot * a.c.max_pages;
+    int page[Y];
+    auto look_up = [&](int u) {
 #pragma unroll
-      for (int y = 0; y < 2; ++y)
+      for (int y = 0; y < Y; ++y) page[y] = table[min(j0 + 16 * (u * Y + y) + n16, s.L - 1) >> a.page_shift];
+    };
+    // (registers for a second block's keys)
+    constexpr bool kAhead = D <= 128 || (NQ == 1 && NP == 1);
+    look_up(0);
+    u32x4 w[Y][D / 64], next[Y][D / 64];
+    float f[Y], next_f[Y];
+    bool there[Y], next_there[Y];
+    auto load = [&](int u) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[y][i] = 0.f;
+      for (int y = 0; y < Y; ++y) {
+        next_there[y] = page[y] >= 0 && page[y] < a.c.n_pages;
+        const size_t block = (size_t)(next_there[y] ? page[y] : 0) * a.c.H_kv + hk;
+        const int row = min(j0 + 16 * (u * Y + y) + n16, s.L - 1) & ((1 << a.page_shift) - 1);
+        const uint8_t* k = a.c.k + (block << a.page_shift) * D + row * D + 16 * g4;
 #pragma unroll
-      for (int c0 = 0; c0 < D; c0 += C) {
-        u32x4 w[2][C / 32];
-        Raw<E> q[C / 16];
-        load_keys<D, C>(a, at, hk, c0, w);
+        for (int c = 0; c < D / 64; ++c) next[y][c] = ldg16(k + 64 * c);
+        next_f[y] = a.c.k_scale[block] * a.scale_log2e;
+      }
+    };
+    if (kAhead) {
+      load(0);
+      look_up(1);
+    }
+#pragma unroll 1
+    for (int u = 0; u < run; ++u) {
+      const int j = j0 + 16 * u * Y;
+      if (!kAhead) load(u);
 #pragma unroll
-        for (int c = 0; c < C / 16; ++c) q[c].load(a.q, q0 + c0 + c / 2 * 32 + 8 * (c & 1));
+      for (int y = 0; y < Y; ++y) {
+        f[y] = next_f[y];
+        there[y] = next_there[y];
 #pragma unroll
-        for (int c = 0; c < C / 16; ++c) {
+        for (int c = 0; c < D / 64; ++c) w[y][c] = next[y][c];
+      }
+      if (kAhead && u + 1 < run) load(u + 1);
+      look_up(u + (kAhead ? 2 : 1));
+      // (rows see more and more keys: the first one's limit is the least)
+      const bool whole = !a.causal || s.L - s.rows + 1 >= min(j + 16 * Y, s.L);
+      float sum[Y];
+#pragma unroll
+      for (int y = 0; y < Y; ++y) sum[y] = 0.f;
+#pragma unroll
+      for (int m = 0; m < NQ; ++m) {
+        f32x4 x[Y];
+#pragma unroll
+        for (int y = 0; y < Y; ++y) x[y] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
           u32x4 qp[NP];
-          q[c].parts(qp);
+          q[m][c].parts(qp);
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
+          for (int y = 0; y < Y; ++y) {
             const u32x4 v = w[y][c / 2];
             const bf16x8 kk = c & 1 ? widen(v[2], v[3], 1.f) : widen(v[0], v[1], 1.f);
 #pragma unroll
             for (int p = NP - 1; p >= 0; --p)
-              x[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, qp[p]), kk, x[y], 0, 0, 0);
+              x[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qp[p]), kk, x[y], 0, 0, 0);
           }
         }
-      }
-      const float nl = live ? row_base(lse) : -INFINITY;
-      float sum[2] = {0.f, 0.f};
+        // register i of a lane is row 4 g4 + i of the 16
+        const float nl_m = row_base(nl[m]);
 #pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) {  // rows 8 i4 .. +7
-        if (8 * i4 < n_rows) {
-          float base[4];
+        for (int i = 0; i < 4; ++i) {
+          const float base = __shfl(nl_m, 4 * g4 + i, 64);
+          const int n = whole ? 0 : __shfl(lim[m], 4 * g4 + i, 64);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) base[q] = __shfl(nl, mfma_row(4 * i4 + q, half), 64);
-          if (whole) {
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-#pragma unroll
-              for (int q = 0; q < 4; ++q) sum[y] += __builtin_amdgcn_exp2f(fmaf(x[y][4 * i4 + q], f[y], base[q]));
-          } else {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const int n = __shfl(lim, mfma_row(4 * i4 + q, half), 64);
-#pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(x[y][4 * i4 + q], f[y], base[q]));
-                sum[y] += j0 + 32 * y + col < n ? e : 0.f;
-              }
-            }
+          for (int y = 0; y < Y; ++y) {
+            const float e = __builtin_amdgcn_exp2f(fmaf(x[y][i], f[y], base));
+            sum[y] += whole || j + 16 * y + n16 < n ? e : 0.f;
           }
         }
       }
 #pragma unroll
-      for (int y = 0; y < 2; ++y) acc[y] += at.there[y] ? sum[y] : 0.f;
+      for (int y = 0; y < Y; ++y) {
+        float e = there[y] ? sum[y] : 0.f;
+        e += __shfl_xor(e, 16, 64);
+        e += __shfl_xor(e, 32, 64);
+        float* to = sums + 16 * (u * Y + y) + n16;
+        if (g4 == 0) *to = first ? e : *to + e;
+      }
     }
+  }
+};
+
+// The waves' sums of tokens [j0, j1), in the waves' order, into the scores; a thread has PER of the old ones.
+template <int PER>
+__device__ __forceinline__ void old_scores(const WeightsArgs& a, const Span2& s, int j0, int j1, float (&was)[PER]) {
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      acc[y] += __shfl_xor(acc[y], 32, 64);
-      if (half == 0) sums[wave][32 * y + col] = acc[y];
+  for (int i = 0; i < PER; ++i) {
+    const int j = j0 + threadIdx.x + i * blockDim.x;
+    was[i] = a.decay != 0.f && j < j1 ? a.score[(size_t)s.slot * a.width + j] : 0.f;
+  }
+}
+template <int PER>
+__device__ __forceinline__ void join_waves(const WeightsArgs& a, const Span2& s, int j0, int j1, const float (&was)[PER],
+                                           int n_waves, const float* sums, int stride) {
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = threadIdx.x + i * blockDim.x;
+    if (j0 + e >= j1) return;
+    float x = 0.f;
+    for (int w = 0; w < n_waves; ++w) x += sums[w * stride + e];
+    a.score[(size_t)s.slot * a.width + j0 + e] = a.decay == 0.f ? x : fmaf(a.decay, was[i], x);
+  }
+}
+
+// Calls of few tokens: 16 to a workgroup, and a wave to each of up to 16 heads.
+template <class E, int D, int NQ>
+__global__ __launch_bounds__(1024) void short_kernel(WeightsArgs a) {
+  __shared__ float sums[16][16];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_waves = blockDim.x >> 6;
+  const int b = blockIdx.x / a.key_blocks, kb = blockIdx.x - b * a.key_blocks, j0 = kb * 16;
+  const Span2 s = sequence(a, b);
+  if (s.slot < 0) return;
+  if (j0 < s.L) {
+    const int j1 = min(j0 + 16, s.L);
+    float was[1];
+    old_scores(a, s, j0, j1, was);
+    if (s.rows == 0 && (threadIdx.x & 63) < 16) sums[wave][threadIdx.x & 15] = 0.f;
+    for (int hk = wave; hk < a.c.H_kv && s.rows > 0; hk += n_waves) {
+      FewRows<E, D, 1, NQ> rows;
+      rows.load(a, s, b, hk);
+      rows.add(a, s, hk, j0, 1, hk == wave, sums[wave]);
     }
     __syncthreads();
-    if (tid < kKeys && j0 + tid < a.width) {
-      const int j = j0 + tid;
-      float x = 0.f;
-      for (int w = 0; w < n_waves; ++w) x += sums[w][tid];
-      if (j < s.L)
-        score[j] = a.decay == 0.f ? x : fmaf(a.decay, score[j], x);
-      else if (a.decay == 0.f)
-        score[j] = 0.f;
+    join_waves(a, s, j0, j1, was, n_waves, &sums[0][0], 16);
+  }
+  if (a.decay != 0.f) return;
+  // zeros behind the sequence
+  float* score = a.score + (size_t)s.slot * a.width;
+  if (threadIdx.x >= 16) return;
+  for (long long j = kb * 16LL + threadIdx.x; j < a.width; j += a.key_blocks * 16LL)
+    if (j >= s.L) score[j] = 0.f;
+}
+
+// The 64-token blocks of all sequences, one after the other, in equal pieces, a
+// workgroup to a piece, as many as the GPU holds at once (kFewPerCu a CU, by the
+// registers).  With a workgroup to every block or four the lengths of the sequences
+// leave a last round that is mostly idle.  More than 8 KV heads take 8 waves (16
+// sequences of 2 k to 8 k tokens, 32 heads: 69 us, 73 with 4; in fp32 51 and 101),
+// fewer 4 (8 heads: 61 us, 62 with 8).
+template <class E, int D, int WAVES, int NQ>
+constexpr int kFewPerCu = WAVES == 8 || (D == 256 && E::kBytes == 4) ? 1 : NQ == 1 && D <= 128 && E::kBytes == 2 ? 3 : 2;
+template <class E, int D, int WAVES, int NQ>
+__global__ __launch_bounds__(64 * WAVES, (kFewPerCu<E, D, WAVES, NQ> * WAVES / 4)) void few_rows_kernel(WeightsArgs a) {
+  constexpr int kPer = (kRun + WAVES - 1) / WAVES;  // tokens of a thread
+  __shared__ float sums[WAVES][64 * kRun];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  auto blocks_of = [&](int b) { return b < a.B ? (sequence(a, b).L + 63) / 64 : 0; };
+  auto scan = [&](int b0) { return wave_incl_scan(blocks_of(b0 + lane), lane); };
+  int ends = scan(0), total = __builtin_amdgcn_readlane(ends, 63);
+  for (int b0 = 64; b0 < a.B; b0 += 64) total += __builtin_amdgcn_readlane(scan(b0), 63);
+  const Cut cut(total, gridDim.x);
+  if ((int)blockIdx.x < cut.n) {
+    int at = cut.start(blockIdx.x);
+    const int end = cut.start(blockIdx.x + 1);
+    int before = 0, b0 = 0;
+    while (before + __builtin_amdgcn_readlane(ends, 63) <= at) {
+      before += __builtin_amdgcn_readlane(ends, 63);
+      b0 += 64;
+      ends = scan(b0);
+    }
+    const int i = __builtin_ctzll(__ballot(before + ends > at));
+    int b = b0 + i, block = at - before - (i ? __builtin_amdgcn_readlane(ends, i - 1) : 0);
+    Span2 s = sequence(a, b);
+    FewRows<E, D, 4, NQ> rows;
+    bool held = false;  // the rows of the wave's first head, if it has no other
+    while (true) {
+      const int left = (s.L + 63) / 64 - block, run = min(min(left, end - at), kRun);
+      const int j0 = block * 64, j1 = min(j0 + 64 * run, s.L);
+      float was[kPer];
+      old_scores(a, s, j0, j1, was);
+      if (s.rows == 0 || wave >= a.c.H_kv)
+        for (int e = lane; e < 64 * kRun; e += 64) sums[wave][e] = 0.f;
+      for (int hk = wave; hk < a.c.H_kv && s.rows > 0; hk += WAVES) {
+        if (!held || a.c.H_kv > WAVES) rows.load(a, s, b, hk);
+        rows.add(a, s, hk, j0, run, hk == wave, sums[wave]);
+      }
+      held = true;
+      __syncthreads();
+      join_waves(a, s, j0, j1, was, WAVES, &sums[0][0], 64 * kRun);
+      at += run;
+      block += run;
+      if (at >= end) break;
+      if (run == left) {  // to the next sequence that has tokens (there is one)
+        do {
+          s = sequence(a, ++b);
+        } while (s.L == 0);
+        block = 0;
+        held = false;
+      }
+      __syncthreads();  // the sums are read before the next ones are written
     }
   }
   if (a.decay != 0.f) return;
-  // the blocks of the row past those that hold tokens
-  const int held = (s.L + kKeys - 1) / kKeys;
-  for (long long j = (kb < held ? (long long)kb + a.key_blocks : kb) * kKeys + tid; j < a.width;
-       j += (long long)a.key_blocks * kKeys)
-    if (tid < kKeys) score[j] = 0.f;
+  // zeros behind the sequences
+  const int per = (a.width + 64 * WAVES - 1) / (64 * WAVES);
+  for (long long e = blockIdx.x; e < (long long)a.B * per; e += gridDim.x) {
+    const int b = (int)(e / per);
+    const long long j = (e - (long long)b * per) * (64 * WAVES) + tid;
+    const Span2 s = sequence(a, b);
+    if (s.slot >= 0 && j >= s.L && j < a.width) a.score[(size_t)s.slot * a.width + j] = 0.f;
+  }
 }
 
 // ----------------------------------------------------------------- many rows
@@ -418,11 +558,22 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(WeightsArgs a) {
 template <class E, int D>
 hipError_t launch(const WeightsArgs& a, const WeightsPlan& p, hipStream_t s) {
   if (p.few) {
-    const dim3 grid((unsigned)(a.B * (long long)a.key_blocks)), block(64 * std::min(a.c.H_kv, kMaxWaves));
-    if (a.c.H_kv <= 4)
-      hipLaunchKernelGGL((few_rows_kernel<E, D, 4>), grid, block, 0, s, a);
-    else
-      hipLaunchKernelGGL((few_rows_kernel<E, D, kMaxWaves>), grid, block, 0, s, a);
+    const long long blocks = (long long)a.B * a.key_blocks;
+    auto go = [&](auto kernel, long long groups, int waves) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(blocks, groups)), dim3(64 * waves), 0, s, a);
+    };
+    auto by_rows = [&](auto nq) {
+      constexpr int NQ = decltype(nq)::value;
+      if (p.tokens == 16)
+        go(short_kernel<E, D, NQ>, blocks, std::min(a.c.H_kv, 16));
+      else
+        a.c.H_kv <= 8 ? go(few_rows_kernel<E, D, 4, NQ>, 256 * kFewPerCu<E, D, 4, NQ>, 4)
+                      : go(few_rows_kernel<E, D, 8, NQ>, 256 * kFewPerCu<E, D, 8, NQ>, 8);
+    };
+    if (a.T_max * a.G <= 16) by_rows(std::integral_constant<int, 1>());
+    if constexpr (E::kBytes == 2) {
+      if (a.T_max * a.G > 16) by_rows(std::integral_constant<int, 2>());
+    }
     return hipGetLastError();
   }
   hipLaunchKernelGGL((many_rows_kernel<E, D>),
@@ -435,11 +586,14 @@ hipError_t launch(const WeightsArgs& a, const WeightsPlan& p, hipStream_t s) {
 
 }  // namespace
 
-WeightsPlan weights_plan(int B, int T_max, int H_kv, int G, int kv_max) {
+WeightsPlan weights_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtype) {
   WeightsPlan p = {};
   const long long n_rows = (long long)T_max * G;
-  p.few = n_rows <= kRows;
-  p.key_blocks = p.few ? (kv_max + kKeys - 1) / kKeys : (kv_max + 4 * kKeys - 1) / (4 * kKeys);
+  // (two tiles of fp32 rows and a block of keys pass the registers)
+  p.few = n_rows <= 16 || (n_rows <= 32 && dtype == TREVS_BF16);
+  // few rows: calls that leave most CUs without a workgroup of 64 tokens take 16 in each
+  p.tokens = !p.few ? 4 * kKeys : (long long)B * kv_max < 64 * 128 ? 16 : 64;
+  p.key_blocks = (kv_max + p.tokens - 1) / p.tokens;
   p.heads = 1;
   p.head_groups = H_kv;
   p.pieces = 1;
