@@ -366,7 +366,10 @@ trevs_status validate_evict(const trevs_kv8_cache* c, const trevs_kv8_evict_args
 size_t evict_info_bytes(const trevs_kv8_evict_args* a) { return align_up((size_t)a->B * sizeof(EvictInfo)); }
 
 // ---------------------------------------------------------------- beam search
-int beam_chunks(const trevs_beam_select_args* a) { return (int)(((int64_t)a->V + kBeamChunk - 1) / kBeamChunk); }
+int beam_chunks(const trevs_beam_select_args* a) {
+  const int chunk = beam_chunk(a->dtype);
+  return (int)(((int64_t)a->V + chunk - 1) / chunk);
+}
 
 trevs_status validate_beam(const trevs_beam_select_args* a) {
   if (!a || a->struct_size != sizeof(trevs_beam_select_args)) return TREVS_ERR_INVALID_ARG;
@@ -674,7 +677,7 @@ trevs_status trevs_pages_reorder(const trevs_kv8_cache* c, int32_t n_groups, int
 
 size_t trevs_beam_select_workspace_size(const trevs_beam_select_args* a) {
   if (validate_beam(a) != TREVS_OK) return 0;
-  return beam_part_bytes(a) + align_up((size_t)a->B * a->W * beam_chunks(a) * a->n_out * sizeof(uint64_t));
+  return beam_part_bytes(a) + align_up((size_t)a->B * a->W * beam_chunks(a) * beam_stride(a->n_out) * sizeof(uint64_t));
 }
 
 trevs_status trevs_beam_select(const trevs_beam_select_args* a, void* ws, size_t ws_bytes, void* stream) {
@@ -696,6 +699,7 @@ trevs_status trevs_beam_select(const trevs_beam_select_args* a, void* ws, size_t
   t.n = a->n_out;
   t.eos = a->eos;
   t.chunks = beam_chunks(a);
+  t.stride = beam_stride(a->n_out);
   TREVS_HIP(launch_beam_select(t, a->dtype, reinterpret_cast<hipStream_t>(stream)));
   return TREVS_OK;
 }

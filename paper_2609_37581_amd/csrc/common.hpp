@@ -200,6 +200,14 @@ __device__ __forceinline__ float key2f(uint32_t k) {
   return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
 }
 
+// A copy of v that the compiler cannot see through, so that compares on it are
+// redone where they are used instead of being kept live (as one 64-bit lane
+// mask per element) across a whole selection.
+__device__ __forceinline__ int opaque(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
 // Workgroup-id remap so that consecutive logical tiles land on the same XCD:
 // the hardware hands workgroup w to XCD (w % 8); XCD x gets the contiguous
 // logical range starting at x*(W/8) + min(x, W%8).

@@ -95,14 +95,6 @@ __device__ __forceinline__ void wave0_find_bin(int krem, SelectShared& sh) {
   __syncthreads();
 }
 
-// A copy of v that the compiler cannot see through, so that compares on it are
-// redone where they are used instead of being kept live (as one 64-bit lane
-// mask per element) across a whole selection.
-__device__ __forceinline__ int opaque(int v) {
-  asm volatile("" : "+v"(v));
-  return v;
-}
-
 // Number of this thread's valid elements: element e is valid iff e < rounds.
 template <int E>
 __device__ __forceinline__ int thread_rounds(int N) {
