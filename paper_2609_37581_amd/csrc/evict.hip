@@ -1,11 +1,10 @@
 // Which tokens of a cached sequence stay: the first and last ones, and of those
 // between the highest scores.
 //
-// One workgroup to a sequence: the choice is a stable top-K (select.hpp) over keys
-// held in registers, E of them a thread, in which the tokens that always stay have
-// the largest key and NaN the smallest.  Bound by latency: the selection's passes
-// over LDS histograms, one after the other.  Sequences longer than its 65,536
-// tokens take a bisection over the keys' bits that reads the scores again each time.
+// One workgroup to a sequence: the choice is a stable top-K over keys held in
+// registers, E of them a thread, in which the tokens that always stay have the largest
+// key and NaN the smallest.  Bound by latency: a count and a barrier for each bit of the
+// key.  Sequences of more than 65,536 tokens read the scores again for each bit.
 #include "cache.hpp"
 #include "select.hpp"
 
@@ -15,22 +14,75 @@ namespace {
 __device__ __forceinline__ uint32_t score_key(float s) { return s != s ? 0u : f2key(s); }
 
 // Calls emit(j, kept, kept tokens before j) for every token j < L, n < L of which are kept.
+// The n-th largest key is found bit by bit, counting with ballots: the scores of a
+// sequence share few exponents, so a histogram's atomics meet (16,547 tokens: the
+// selection of select.hpp 25 us, this way 12).
 template <int E, class Emit>
 __device__ __forceinline__ void select_held(const float* score, int L, int n, int first, int last, Emit emit,
                                             SelectShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   uint32_t key[E];
 #pragma unroll
+  for (int e = 0; e < E; ++e) key[e] = score_key(score[min(e * kSelThreads + tid, L - 1)]);
+#pragma unroll
   for (int e = 0; e < E; ++e) {
-    const int j = e * kSelThreads + (int)threadIdx.x;
-    key[e] = score_key(score[min(j, L - 1)]);
+    const int j = e * kSelThreads + tid;
     if (j < first || j >= L - last) key[e] = 0xffffffffu;
+    if (j >= L) key[e] = 0u;  // (as NaN, but never emitted; nothing is counted by a bound of 0)
   }
-  block_topk_each<E>(
-      key, L, n,
-      [&](int e, bool ok, bool keep, int before) {
-        if (ok) emit(e * kSelThreads + (int)threadIdx.x, keep, before);
-      },
-      sh, false, 0u, 0u);
+  uint32_t thr = 0;
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t least = thr | (1u << bit);
+    int count = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) count += __popcll(__ballot(key[e] >= least));
+    uint32_t* counts = sh.wcnt + (bit & 1) * kSelWaves;
+    if (lane == 0) counts[wave] = (uint32_t)count;
+    __syncthreads();
+    const int total = __builtin_amdgcn_readlane(wave_incl_scan((int)counts[lane & (kSelWaves - 1)], lane), kSelWaves - 1);
+    if (total >= n) thr = least;
+    if (total == n) break;
+  }
+  __syncthreads();  // the counts are read before the words below are written
+  // above the threshold, and equal to it, before each token
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const bool in = e * kSelThreads + tid < L;
+    const uint64_t above = __ballot(in && key[e] > thr), ties = __ballot(in && key[e] == thr);
+    if (lane == 0) sh.wcnt[e * kSelWaves + wave] = (uint32_t)__popcll(above) | ((uint32_t)__popcll(ties) << 16);
+  }
+  __syncthreads();
+  // (packed sums of up to 65,536 of either: each half's exclusive ones fit it, the sum of all `above` is n at most)
+  if (wave == 0) {
+    constexpr int kPer = (E * kSelWaves + 63) / 64;
+    uint32_t c[kPer], sum = 0;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      const int i = lane * kPer + q;
+      c[q] = i < E * kSelWaves ? sh.wcnt[i] : 0u;
+      sum += c[q];
+    }
+    uint32_t run = wave_incl_scan_u32(sum) - sum;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      const int i = lane * kPer + q;
+      if (i < E * kSelWaves) sh.wcnt[i] = run;
+      run += c[q];
+    }
+    if (lane == 63) sh.total = (int)(run & 0xffffu);
+  }
+  __syncthreads();
+  const int need = n - sh.total;  // ties kept, lowest index first
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int j = e * kSelThreads + tid;
+    const bool in = j < L, over = in && key[e] > thr, tie = in && key[e] == thr;
+    const uint64_t below = (1ull << lane) - 1;
+    const uint32_t base = sh.wcnt[e * kSelWaves + wave];
+    const int na = (int)(base & 0xffffu) + __popcll(__ballot(over) & below);
+    const int nt = (int)(base >> 16) + __popcll(__ballot(tie) & below);
+    if (in) emit(j, over || (tie && nt < need), na + min(nt, need));
+  }
 }
 
 // The same for any length: a thread owns `per` tokens in a row.
@@ -95,8 +147,10 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) 
     select_held<1>(score, L, n, a.n_first, a.n_last, emit, sh);
   else if (L <= 4 * kSelThreads)
     select_held<4>(score, L, n, a.n_first, a.n_last, emit, sh);
-  else if (L <= 16 * kSelThreads)
-    select_held<16>(score, L, n, a.n_first, a.n_last, emit, sh);
+  else if (L <= 12 * kSelThreads)
+    select_held<12>(score, L, n, a.n_first, a.n_last, emit, sh);
+  else if (L <= 20 * kSelThreads)
+    select_held<20>(score, L, n, a.n_first, a.n_last, emit, sh);
   else if (L <= 32 * kSelThreads)
     select_held<32>(score, L, n, a.n_first, a.n_last, emit, sh);
   else if (L <= TREVS_MAX_SELECT_N)
