@@ -342,11 +342,18 @@ __global__ __launch_bounds__(64 * WAVES, (kFewPerCu<E, D, WAVES, NQ> * WAVES / 4
 
 // ----------------------------------------------------------------- many rows
 // A workgroup's four waves hold 64 keys each, widened once into registers, while the
-// query rows of a group, r = t G + g, pass by 32 at a time, staged in LDS a step ahead.
-// Its sums are one of the `splits` parts of its keys' scores, joined by sum_kernel.
+// query rows of a group, r = t G + g, pass by, staged in LDS a step ahead.  Its sums are
+// one of the parts of its keys' scores, joined by sum_kernel.  Bound by the vector units
+// and the matrix cores one after the other: of a pass over prompts of 4 x 4259 rows with
+// 28/4 heads of 128 (325 us, 800 TFLOP/s) the former are busy 58 % of the cycles, a third
+// of that with exponentials, the latter 43 %, and hardly any at the same time, also where
+// the exponentials of one product are placed among the instructions of the next (344 us).
+// Permutation of a staged row's 16-byte columns, by the row's low bits reversed: 16 lanes
+// next to each other read one column of 16 rows, or write 4 or 8 columns of 4 or 2 rows,
+// and meet 16 different ones modulo 256 bytes, the width of the banks, either way.
 template <int D>
 __device__ __forceinline__ int query_swizzle(int row) {
-  return D == 64 ? (row >> 1) & 7 : row & 15;
+  return (int)(D == 64 ? __brev((uint32_t)row >> 1) >> 29 : __brev((uint32_t)row) >> 28);
 }
 
 // Rows staged at once: two products' for bf16 rows of up to 128 channels.
@@ -412,33 +419,29 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void many_rows_kernel(Weight
   const Places at_keys(a, s, jw);
   for (int hk = hg * a.heads; hk < min((hg + 1) * a.heads, a.c.H_kv); ++hk) {
     if (first >= end) break;
-    // A thread stages the same 8 channels of every S-th row: it follows its rows' places.  (Dividing each
-    // row's number by G takes as long as the exponentials.)
+    // A thread stages parts of every S-th row: it follows the row's place.  (Dividing the row's number by G
+    // takes as long as the exponentials.)
+    constexpr int kPer = 256 / S;  // threads of a row, which has kPer * kVecs vectors
+    static_assert(kPer * kVecs == D / 8, "whole rows");
     Raw<E> raw[kVecs];
-    const size_t head = ((size_t)b * a.T_max) * a.q_ld + (size_t)hk * a.G * D;
     const long long step = (long long)(S / a.G) * a.q_ld + S % a.G * D, wrap = a.q_ld - (long long)a.G * D;
-    size_t at[kVecs];
-    int g[kVecs], row = first * S + tid / (D / 8);  // (of vector 0; the others' lie 256 / (D / 8) rows on)
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int r = row + i * (256 * 8 / D), t = r / a.G;
-      g[i] = r - t * a.G;
-      at[i] = head + (size_t)t * a.q_ld + g[i] * D + tid % (D / 8) * 8;
-    }
+    const int in_row = tid / kPer, vec = tid % kPer;
+    int row = first * S + in_row, g = row % a.G;
+    const size_t head = (size_t)b * a.T_max * a.q_ld + (size_t)hk * a.G * D + vec * 8;
+    size_t at = head + (size_t)(row / a.G) * a.q_ld + g * D;
     float base = 0.f;
     int lim = 0;
     auto load = [&](int stage) {
+      // (a row past the last is the first one: its weights come to nothing, but it may hold anything)
+      const size_t from = row < n_rows ? at : head;
 #pragma unroll
-      for (int i = 0; i < kVecs; ++i) {
-        // (a row past the last is the first one: its weights come to nothing, but it may hold anything)
-        raw[i].load(a.q, row + i * (256 * 8 / D) < n_rows ? at[i] : head + tid % (D / 8) * 8);
-        at[i] += step;
-        g[i] += S % a.G;
-        const bool over = g[i] >= a.G;
-        at[i] += over ? wrap : 0;
-        g[i] -= over ? a.G : 0;
-      }
+      for (int i = 0; i < kVecs; ++i) raw[i].load(a.q, from + i * (kPer * 8));
       row += S;
+      at += step;
+      g += S % a.G;
+      const bool over = g >= a.G;
+      at += over ? wrap : 0;
+      g -= over ? a.G : 0;
       if (tid < S) {
         const int r = stage * S + tid, t = r / a.G, h = hk * a.G + r - t * a.G;
         base = r < n_rows ? row_base(a.lse[((size_t)b * a.H_q + h) * a.T_max + t]) : -INFINITY;
@@ -448,11 +451,11 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void many_rows_kernel(Weight
     auto store = [&](int buf) {
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) {
-        const int e = tid + 256 * i, r = e / (D / 8), c = e % (D / 8);
         u32x4 parts[NP];
         raw[i].parts(parts);
 #pragma unroll
-        for (int p = 0; p < NP; ++p) sh.q[buf][p][r * (D / 8) + (c ^ query_swizzle<D>(r))] = parts[p];
+        for (int p = 0; p < NP; ++p)
+          sh.q[buf][p][in_row * (D / 8) + ((vec + i * kPer) ^ query_swizzle<D>(in_row))] = parts[p];
       }
       if (tid < S) {
         reinterpret_cast<float*>(sh.base[buf])[tid] = base;
@@ -598,8 +601,10 @@ WeightsPlan weights_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtyp
   p.head_groups = H_kv;
   p.pieces = 1;
   if (p.few) return p;
-  const long long row_tiles = (n_rows + kRows - 1) / kRows, want = 2048;
-  // the parts' floats: 64 MB at most, where splitting the heads alone does not pass that
+  // Two workgroups of a CU at once, and as many again for those that see fewer rows (with twice as many prompts
+  // of 4 x 2048 rows with 8/1 heads of 256 take 94 us for 83, of 28/4 of 128 in fp32 104 for 103, the others
+  // the same); the parts' floats: 64 MB at most, where splitting the heads alone does not pass that.
+  const long long row_tiles = (n_rows + kRows - 1) / kRows, want = 1024;
   const long long most = std::max((16LL << 20) / ((long long)B * kv_max), 1LL);
   if (most < H_kv) {
     p.heads = (int)((H_kv + most - 1) / most);
