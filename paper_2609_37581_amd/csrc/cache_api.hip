@@ -382,7 +382,9 @@ trevs_status validate_beam(const trevs_beam_select_args* a) {
       !aligned(a->parent, 4) || !aligned(a->token, 4))
     return TREVS_ERR_INVALID_ARG;
   if (a->W > TREVS_MAX_BEAMS || a->n_out > TREVS_MAX_BEAM_OUT || a->logits_ld > INT32_MAX) return TREVS_ERR_UNSUPPORTED;
-  if ((int64_t)a->W * a->V > INT32_MAX || (int64_t)a->B * a->W > INT32_MAX) return TREVS_ERR_UNSUPPORTED;
+  // (places up to a chunk past the vocabulary stay in 32 bits)
+  if ((int64_t)a->W * a->V > INT32_MAX - beam_chunk(a->dtype) || (int64_t)a->B * a->W > INT32_MAX)
+    return TREVS_ERR_UNSUPPORTED;
   const int64_t rows = (int64_t)a->B * a->W, ld = a->logits_ld ? a->logits_ld : a->V;
   if (rows > kMaxGroups / beam_chunks(a) || a->B > kMaxGroups / 4) return TREVS_ERR_UNSUPPORTED;
   const size_t list = (size_t)a->B * a->n_out * 4;

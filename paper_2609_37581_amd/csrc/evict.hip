@@ -4,7 +4,7 @@
 // One workgroup to a sequence: the choice is a stable top-K over keys held in
 // registers, E of them a thread, in which the tokens that always stay have the largest
 // key and NaN the smallest.  Bound by latency: a count and a barrier for each bit of the
-// key.  Sequences of more than 65,536 tokens read the scores again for each bit.
+// key.  Sequences of more than 32,768 tokens read the scores again for each bit.
 #include "cache.hpp"
 #include "select.hpp"
 
@@ -14,9 +14,10 @@ namespace {
 __device__ __forceinline__ uint32_t score_key(float s) { return s != s ? 0u : f2key(s); }
 
 // Calls emit(j, kept, kept tokens before j) for every token j < L, n < L of which are kept.
-// The n-th largest key is found bit by bit, counting with ballots: the scores of a
-// sequence share few exponents, so a histogram's atomics meet (16,547 tokens: the
-// selection of select.hpp 25 us, this way 12).
+// The n-th largest key is found bit by bit (few keys a thread: two bits), counting with
+// ballots: the scores of a sequence share few exponents, so a histogram's atomics would
+// meet in few bins (up to 16,547 tokens: the selection of select.hpp 25 us, this way 22.5;
+// up to 700 tokens 10, which the loads that wait for each other take).
 template <int E, class Emit>
 __device__ __forceinline__ void select_held(const float* score, int L, int n, int first, int last, Emit emit,
                                             SelectShared& sh) {
@@ -30,18 +31,35 @@ __device__ __forceinline__ void select_held(const float* score, int L, int n, in
     if (j < first || j >= L - last) key[e] = 0xffffffffu;
     if (j >= L) key[e] = 0u;  // (as NaN, but never emitted; nothing is counted by a bound of 0)
   }
+  // BITS bits of the threshold at a time: the keys that reach each of the values that they can have
+  constexpr int BITS = E <= 4 ? 2 : 1, kSteps = 32 / BITS, kValues = (1 << BITS) - 1;
+  for (int i = tid; i < kSteps * kValues; i += kSelThreads) sh.hist[i] = 0u;
+  __syncthreads();
   uint32_t thr = 0;
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t least = thr | (1u << bit);
-    int count = 0;
+  for (int step = 0; step < kSteps; ++step) {
+    const int shift = 32 - BITS * (step + 1);
+    int count[kValues] = {};
 #pragma unroll
-    for (int e = 0; e < E; ++e) count += __popcll(__ballot(key[e] >= least));
-    uint32_t* counts = sh.wcnt + (bit & 1) * kSelWaves;
-    if (lane == 0) counts[wave] = (uint32_t)count;
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int v = 0; v < kValues; ++v) count[v] += __popcll(__ballot(key[e] >= (thr | ((v + 1u) << shift))));
+    uint32_t* counts = sh.hist + step * kValues;
+#pragma unroll
+    for (int v = 0; v < kValues; ++v)
+      if (lane == v) atomicAdd(&counts[v], (uint32_t)count[v]);
     __syncthreads();
-    const int total = __builtin_amdgcn_readlane(wave_incl_scan((int)counts[lane & (kSelWaves - 1)], lane), kSelWaves - 1);
-    if (total >= n) thr = least;
-    if (total == n) break;
+    uint32_t digit = 0;
+    bool exact = false;
+#pragma unroll
+    for (int v = 0; v < kValues; ++v) {
+      const int total = __builtin_amdgcn_readfirstlane((int)counts[v]);
+      if (total >= n) {
+        digit = v + 1;
+        exact = total == n;
+      }
+    }
+    thr |= digit << shift;
+    if (exact) break;
   }
   __syncthreads();  // the counts are read before the words below are written
   // above the threshold, and equal to it, before each token
@@ -91,15 +109,16 @@ __device__ void select_streamed(const float* score, int L, int n, int first, int
   const int per = (L + kSelThreads - 1) / kSelThreads;
   const int j0 = (int)min((long long)threadIdx.x * per, (long long)L), j1 = min(j0 + per, L);
   auto key = [&](int j) { return j < first || j >= L - last ? 0xffffffffu : score_key(score[j]); };
-  auto count = [&](uint32_t least) {
-    int c = 0, total;
-    for (int j = j0; j < j1; ++j) c += key(j) >= least;
-    block_excl_scan(c, sh, total);
-    return total;
-  };
   uint32_t thr = 0;  // the n-th largest key
-  for (int bit = 31; bit >= 0; --bit)
-    if (count(thr | (1u << bit)) >= n) thr |= 1u << bit;
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t least = thr | (1u << bit);
+    int c = 0, total;
+#pragma unroll 8
+    for (int j = threadIdx.x; j < L; j += kSelThreads) c += key(j) >= least;
+    block_excl_scan(c, sh, total);
+    if (total >= n) thr = least;
+    if (total == n) break;
+  }
   int above = 0, ties = 0, n_above, n_ties;
   for (int j = j0; j < j1; ++j) {
     const uint32_t k = key(j);
@@ -153,8 +172,6 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) 
     select_held<20>(score, L, n, a.n_first, a.n_last, emit, sh);
   else if (L <= 32 * kSelThreads)
     select_held<32>(score, L, n, a.n_first, a.n_last, emit, sh);
-  else if (L <= TREVS_MAX_SELECT_N)
-    select_held<64>(score, L, n, a.n_first, a.n_last, emit, sh);
   else
     select_streamed(score, L, n, a.n_first, a.n_last, emit, sh);
   if (gone != INT32_MAX) atomicMin(&s_first, gone);

@@ -105,7 +105,8 @@ def test_evict_rejects_before_launch(bad, code):
     (dict(logits=ptr(20, 1)), 1), (dict(dtype=trevs.TREVS_F32, logits=ptr(20, 2)), 1), (dict(score=None), 1),
     (dict(done=ptr(25, 2)), 1), (dict(score_out=None), 1), (dict(parent=ptr(23, 2)), 1), (dict(token=None), 1),
     (dict(token=ptr(23, 32)), 1), (dict(parent=ptr(20, 64)), 1), (dict(done=ptr(24)), 1), (dict(W=65), 2),
-    (dict(n_out=65), 2), (dict(W=64, V=1 << 26), 2), (dict(B=1 << 22, W=64, V=100000), 2),
+    (dict(n_out=65), 2), (dict(W=64, V=1 << 26), 2), (dict(W=1, V=(1 << 31) - 2000), 2),
+    (dict(B=1 << 22, W=64, V=100000), 2),
     (dict(logits_ld=1 << 32), 2),
 ])
 def test_beam_select_rejects_before_launch(bad, code):
