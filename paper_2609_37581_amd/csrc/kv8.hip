@@ -378,7 +378,7 @@ __global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void compact_kernel(Com
 
 // Eviction's rows into their new pages: block (layer, b, f, h) of request b as its
 // kept tokens say (evict_select_kernel, evict_pages_kernel); the old pages are in
-// `old`, since the table has the new ones already.  The last B workgroups (of keys)
+// `old`, since the table has the new ones already.  The last B workgroups (of values)
 // do what no block depends on any more: the old pages' counts, the table's end, the
 // length, and the scores, which move down in place, each round's reads before its writes.
 template <int D, int PAGE>
@@ -419,15 +419,19 @@ __device__ __forceinline__ void evict_finish(const EvictArgs& a, const EvictInfo
   for (int i = e.n + tid; i < e.len; i += NT) score[i] = 0.f;
 }
 
+// (Values, which read every page from the first loss on, go before keys, and 6 waves share
+// a SIMD's registers: 4 layers of 4 sequences of 4.3 k to 16.5 k tokens cut to 2048, 4
+// heads of 128, 39 us; keys first and 5 waves 46.  HBM's share, with all value bytes, is
+// 27 us; the rest is each block's chain of source pages.)
 template <int D, int PAGE, bool TURNS>
-__global__ __launch_bounds__((Block<D, PAGE>::kThreads)) void evict_kernel(EvictArgs a) {
+__global__ __launch_bounds__((Block<D, PAGE>::kThreads), D <= 128 && !TURNS ? 6 : 1) void evict_kernel(EvictArgs a) {
   __shared__ MoveShared<D, PAGE> sh;
-  const bool values = blockIdx.y != 0;
+  const bool values = blockIdx.y == 0;
   const int tid = threadIdx.x;
   unsigned id = blockIdx.x;
   const unsigned moves = gridDim.x - a.B;
   if (id >= moves) {
-    if (!values) evict_finish<D, PAGE>(a, a.info[id - moves], id - moves);
+    if (values) evict_finish<D, PAGE>(a, a.info[id - moves], id - moves);
     return;
   }
   const int h = (int)(id % a.c.H_kv);
