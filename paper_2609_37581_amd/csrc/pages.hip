@@ -358,22 +358,26 @@ __device__ __forceinline__ void read_group(const PagesArgs& a, int g, int width,
 constexpr int kReorderThreads = 128;
 constexpr int kReorderHeld = TREVS_MAX_BEAMS * kReorderThreads;  // entries that a workgroup holds
 
-// A thread holds a column of the group, so reads are done before writes.
+// A thread holds a column of the group, so reads are done before writes.  (The columns lie
+// in as much LDS as the beams need, or too few workgroups fit a CU: 16 x 8 beams of 1.3 k to
+// 16.6 k tokens 7.6 us, 12.6 with room for 64.)
 __global__ __launch_bounds__(kReorderThreads) void reorder_scores_kernel(PagesArgs a, int width, const int32_t* slots,
                                                                          const int32_t* parent, float* score) {
   __shared__ Group s;
-  __shared__ float held[TREVS_MAX_BEAMS][kReorderThreads];
+  extern __shared__ float held_scores[];
   const int tid = threadIdx.x, g = blockIdx.y;
   read_group(a, g, width, slots, parent, s);
   int longest = 0;
   for (int w = 0; w < width; ++w) longest = max(longest, s.len[w]);
   const size_t row = (size_t)a.max_pages << a.page_shift;
+  float* held = held_scores + tid;
   for (int j = blockIdx.x * kReorderThreads + tid; j < longest; j += gridDim.x * kReorderThreads) {
 #pragma unroll 8
-    for (int w = 0; w < width; ++w) held[w][tid] = s.slot[w] >= 0 ? score[s.slot[w] * row + j] : 0.f;
+    for (int w = 0; w < width; ++w) held[w * kReorderThreads] = s.slot[w] >= 0 ? score[s.slot[w] * row + j] : 0.f;
     for (int w = 0; w < width; ++w) {
       const int p = s.src[w];
-      if (p != w && j < max(s.len[w], s.len[p])) score[s.slot[w] * row + j] = j < s.len[p] ? held[p][tid] : 0.f;
+      if (p != w && j < max(s.len[w], s.len[p]))
+        score[s.slot[w] * row + j] = j < s.len[p] ? held[p * kReorderThreads] : 0.f;
     }
   }
 }
@@ -428,8 +432,8 @@ hipError_t launch_pages_reorder(const PagesArgs& a, int groups, int width, const
   if (score) {
     const long long tokens = (long long)a.max_pages << a.page_shift;
     const int blocks = (int)min((tokens + kReorderThreads - 1) / kReorderThreads, 4096LL / groups + 1);
-    hipLaunchKernelGGL(reorder_scores_kernel, dim3(blocks, groups), dim3(kReorderThreads), 0, s, a, width, slots,
-                       parent, score);
+    hipLaunchKernelGGL(reorder_scores_kernel, dim3(blocks, groups), dim3(kReorderThreads),
+                       width * kReorderThreads * sizeof(float), s, a, width, slots, parent, score);
   }
   int threads = 1024;
   while (threads * width > kReorderHeld || (threads > 64 && threads >= 2 * a.max_pages)) threads >>= 1;
