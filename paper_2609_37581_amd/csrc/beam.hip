@@ -76,7 +76,9 @@ __device__ __forceinline__ uint32_t nth_bound(uint32_t v, int n) {
 // m the chunk's maximum: one instruction to an argument.  What L lacks of log2 e makes
 // all of them too small by a factor of about 2^(kRest m), which the join puts back (the
 // terms far from m, where it is another, hardly count), so that continuations of different
-// beams compare as if it were not there.
+// beams compare as if it were not there.  Far from 0 base(m) would be off by whole powers of
+// two: there they are exp2((x - m) L).
+constexpr float kFar = 65536.f;
 constexpr double kRest = 1.4426950408889634073599 - (double)kLog2e;
 __device__ __forceinline__ float chunk_base(float m) { return m * kLog2e; }
 
@@ -205,6 +207,14 @@ __global__ __launch_bounds__(256, E::kBytes == 2 ? 8 : 4) void beam_chunk_kernel
         count += __popcll(hits);
       }
     }
+  if (fabsf(top) >= kFar && top != -INFINITY) {
+    sum[0] = sum[1] = 0.f;
+    c.forget();
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k)
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) sum[e & 1] += __builtin_amdgcn_exp2f((c.x[k][e] - top) * kLog2e);
+  }
   const float total = wave_sum(sum[0] + sum[1]);
   uint64_t* out = a.cand + (size_t)id * a.stride;
   if (count <= a.stride) {
@@ -312,7 +322,9 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
     double sum = 0.0;
     for (int c = lane; c < a.chunks; c += 64) {
       const float2 p = a.part[(size_t)row * a.chunks + c];
-      sum += p.x == -INFINITY && p.y == 0.f ? 0.0 : p.y * exp2(chunk_base(p.x) + kRest * p.x - m * (kLog2e + kRest));
+      const double to = m * (kLog2e + kRest);
+      const double from = fabsf(p.x) >= kFar ? p.x * (kLog2e + kRest) : chunk_base(p.x) + kRest * p.x;
+      sum += p.x == -INFINITY && p.y == 0.f ? 0.0 : p.y * exp2(from - to);
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);

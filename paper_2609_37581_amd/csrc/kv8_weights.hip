@@ -19,11 +19,11 @@ namespace {
 constexpr int kKeys = 64;   // keys of a wave: two columns of 32 a lane
 constexpr int kRows = 32;   // query rows of a product
 
-struct Span2 {
+struct Seq {
   int slot, rows, L;
 };
-__device__ __forceinline__ Span2 sequence(const WeightsArgs& a, int b) {
-  Span2 s;
+__device__ __forceinline__ Seq sequence(const WeightsArgs& a, int b) {
+  Seq s;
   s.slot = slot_of(a.slots, b, a.c.n_slots);
   s.rows = a.q_len ? min(max(a.q_len[b], 0), a.T_max) : a.T_max;
   s.L = slot_len(a.c.len, s.slot, a.kv_max);
@@ -63,7 +63,7 @@ struct Places {
   size_t block[2];  // page, counted in KV heads' blocks
   int row[2];       // in the page
   bool there[2];
-  __device__ __forceinline__ Places(const WeightsArgs& a, const Span2& s, int j0) {
+  __device__ __forceinline__ Places(const WeightsArgs& a, const Seq& s, int j0) {
     const int col = threadIdx.x & 31;
     const int32_t* table = a.c.table + (size_t)max(s.slot, 0) * a.c.max_pages;
     int page[2];
@@ -108,7 +108,7 @@ struct FewRows {
   Raw<E> q[NQ][D / 32];
   float nl[NQ];  // of row 16 m + lane % 16
   int lim[NQ];
-  __device__ __forceinline__ void load(const WeightsArgs& a, const Span2& s, int b, int hk) {
+  __device__ __forceinline__ void load(const WeightsArgs& a, const Seq& s, int b, int hk) {
     const int n16 = threadIdx.x & 15, g4 = (threadIdx.x & 63) >> 4, n_rows = s.rows * a.G;
 #pragma unroll
     for (int m = 0; m < NQ; ++m) {
@@ -124,7 +124,7 @@ struct FewRows {
       lim[m] = a.causal ? s.L - s.rows + t + 1 : s.L;
     }
   }
-  __device__ __forceinline__ void add(const WeightsArgs& a, const Span2& s, int hk, int j0, int run, bool first,
+  __device__ __forceinline__ void add(const WeightsArgs& a, const Seq& s, int hk, int j0, int run, bool first,
                                       float* sums) {
     typedef float f32x4 __attribute__((ext_vector_type(4)));
     constexpr int NP = kParts<E>;
@@ -220,7 +220,7 @@ struct FewRows {
 
 // The waves' sums of tokens [j0, j1), in the waves' order, into the scores; a thread has PER of the old ones.
 template <int PER>
-__device__ __forceinline__ void old_scores(const WeightsArgs& a, const Span2& s, int j0, int j1, float (&was)[PER]) {
+__device__ __forceinline__ void old_scores(const WeightsArgs& a, const Seq& s, int j0, int j1, float (&was)[PER]) {
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int j = j0 + threadIdx.x + i * blockDim.x;
@@ -228,7 +228,7 @@ __device__ __forceinline__ void old_scores(const WeightsArgs& a, const Span2& s,
   }
 }
 template <int PER>
-__device__ __forceinline__ void join_waves(const WeightsArgs& a, const Span2& s, int j0, int j1, const float (&was)[PER],
+__device__ __forceinline__ void join_waves(const WeightsArgs& a, const Seq& s, int j0, int j1, const float (&was)[PER],
                                            int n_waves, const float* sums, int stride) {
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(1024) void short_kernel(WeightsArgs a) {
   __shared__ float sums[16][16];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_waves = blockDim.x >> 6;
   const int b = blockIdx.x / a.key_blocks, kb = blockIdx.x - b * a.key_blocks, j0 = kb * 16;
-  const Span2 s = sequence(a, b);
+  const Seq s = sequence(a, b);
   if (s.slot < 0) return;
   if (j0 < s.L) {
     const int j1 = min(j0 + 16, s.L);
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(64 * WAVES, (kFewPerCu<E, D, WAVES, NQ> * WAVES / 4
     }
     const int i = __builtin_ctzll(__ballot(before + ends > at));
     int b = b0 + i, block = at - before - (i ? __builtin_amdgcn_readlane(ends, i - 1) : 0);
-    Span2 s = sequence(a, b);
+    Seq s = sequence(a, b);
     FewRows<E, D, 4, NQ> rows;
     bool held = false;  // the rows of the wave's first head, if it has no other
     while (true) {
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(64 * WAVES, (kFewPerCu<E, D, WAVES, NQ> * WAVES / 4
   for (long long e = blockIdx.x; e < (long long)a.B * per; e += gridDim.x) {
     const int b = (int)(e / per);
     const long long j = (e - (long long)b * per) * (64 * WAVES) + tid;
-    const Span2 s = sequence(a, b);
+    const Seq s = sequence(a, b);
     if (s.slot >= 0 && j >= s.L && j < a.width) a.score[(size_t)s.slot * a.width + j] = 0.f;
   }
 }
@@ -348,6 +348,7 @@ __global__ __launch_bounds__(64 * WAVES, (kFewPerCu<E, D, WAVES, NQ> * WAVES / 4
 // 28/4 heads of 128 (325 us, 800 TFLOP/s) the former are busy 58 % of the cycles, a third
 // of that with exponentials, the latter 43 %, and hardly any at the same time, also where
 // the exponentials of one product are placed among the instructions of the next (344 us).
+
 // Permutation of a staged row's 16-byte columns, by the row's low bits reversed: 16 lanes
 // next to each other read one column of 16 rows, or write 4 or 8 columns of 4 or 2 rows,
 // and meet 16 different ones modulo 256 bytes, the width of the banks, either way.
@@ -406,7 +407,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void many_rows_kernel(Weight
   const int group = blockIdx.x % groups, rest = blockIdx.x / groups;
   const int b = group / a.head_groups, hg = group - b * a.head_groups;
   const int piece = rest % a.pieces, kb = rest / a.pieces;
-  const Span2 s = sequence(a, b);
+  const Seq s = sequence(a, b);
   const int j0 = kb * 4 * kKeys, jw = j0 + wave * kKeys;
   if (s.slot < 0 || j0 >= s.L) return;
   const int n_rows = s.rows * a.G;
@@ -541,7 +542,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void many_rows_kernel(Weight
 constexpr int kSumThreads = 256;
 __global__ __launch_bounds__(kSumThreads) void sum_kernel(WeightsArgs a) {
   const int b = blockIdx.y;
-  const Span2 s = sequence(a, b);
+  const Seq s = sequence(a, b);
   if (s.slot < 0) return;
   const int splits = a.head_groups * a.pieces;
   const float* part = a.part + (size_t)b * splits * a.kv_max;

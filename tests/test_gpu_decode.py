@@ -513,6 +513,20 @@ def test_beam_select_does_not_depend_on_where_rows_lie():
         assert len(set(got[2].flatten().tolist())) == 1
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shift", [0.0, 7e4, -7e4, 1e9, -3e30, 2e38])
+def test_beam_select_logits_far_from_zero(dtype, shift):
+    """Logits up to the largest floats, beside beams of ordinary ones; chunks of either kind in one beam."""
+    rng = np.random.default_rng(9)
+    x = rng.normal(size=(2, 3, 9000)) * max(1.0, abs(shift) / 4) + shift
+    x = x.clip(-3.3e38, 3.3e38)
+    x[0, 1] = rng.normal(size=9000)
+    x[1, 2, :4500] = rng.normal(size=4500)
+    logits, xs = storage(x, dtype)
+    score, s = storage(np.array([[-1.0, -2.0, -0.5], [-3.0, -1.0, -2.0]]), torch.float32)
+    check_beams(trevs.beam_select(logits, score, n_out=9), xs, s, None, 9, 0)
+
+
 def test_beam_select_more_ties_than_the_join_lists():
     """Every listed continuation of 64 beams ties."""
     score = torch.zeros(2, 64, device="cuda")
