@@ -232,7 +232,7 @@ __global__ __launch_bounds__(256, E::kBytes == 2 ? 8 : 4) void beam_chunk_kernel
 }
 
 // ---------------------------------------------------------------------- join
-constexpr int kJoinThreads = 1024;
+constexpr int kJoinThreads = 512;
 constexpr int kJoinList = 1024;
 constexpr int kJoinChunks = 1024;
 
