@@ -563,7 +563,9 @@ trevs_status trevs_kv8_compact(const trevs_kv8_cache* cache, const trevs_kv8_com
 
 /* Scores of cached tokens: the attention weights that they have been given.  score
  * [n_slots, max_pages * page_tokens] holds a number for every token of every slot
- * (the caller's; zeros for an empty slot, and past a slot's length).  One call adds
+ * (the caller's; zeros for an empty slot, and past a slot's length: trevs_pages_fork
+ * and trevs_pages_free leave scores alone, so a fork's are copied and those of tokens
+ * given up are zeroed by the caller).  One call adds
  * the weights of one layer's query rows, all heads summed: for j < L = len[slot]
  *   score[slot][j] = decay score[slot][j] + sum_{h, t < q_len[b], j seen by t}
  *                    exp(scale q[b,t,h] . k_j - lse[b,h,t])

@@ -184,7 +184,8 @@ __device__ __forceinline__ float head_sum(float v) {
 
 // A head's LANES lanes hold two vectors of it each (of the rotated part those whose
 // pairs meet), so the norm's sum of squares is theirs, and every value is read and
-// written once: bound by bytes, as the rotation alone.
+// written once: bound by bytes, as the rotation alone (4 x 4259 rows of 32 heads of 128 in
+// bf16 58.7 us, 4.8 TB/s, the rotation 56.5; a copy of the bytes 54).
 template <class E, bool INTER, int D>
 __global__ __launch_bounds__(kThreads) void norm_rope_kernel(NormRopeArgs n, int rows_per_block) {
   constexpr int VE = Vec<E>::VE, LANES = D / (2 * VE);

@@ -1061,7 +1061,9 @@ class Kv8Weights:
     tokens of one layer, summed over rows and heads and added to decay * score,
     in place.  lse [B,H_q,T] is Kv8Attention's for the same q, q_len, slots,
     layer, causal, scale and kv_max; slots name no slot twice.  decay=0 begins
-    a slot's scores anew.  call() enqueues and returns score."""
+    a slot's scores anew (PagesFork and PagesFree leave them alone: copy a
+    fork's, and zero those of tokens given up).  call() enqueues and returns
+    score."""
 
     def __init__(self, cache, q, lse, score, q_len=None, slots=None, *, layer=0, causal=True, scale=None,
                  kv_max=0, decay=1.0):
