@@ -102,6 +102,19 @@ def test_norm_rope_magnitudes(dtype, d):
         assert (got[0, 5] == 0).all()
 
 
+def test_norm_rope_offsets_past_32_bits():
+    """The last rows of 4.6 GB, in place, give the bits that they give alone."""
+    S, H, d = 140000, 32, 256
+    q = torch.zeros(1, S, H, d, device="cuda")
+    rows, _ = storage(np.random.default_rng(3).normal(size=(1, 7, H, d)), torch.float32)
+    q[:, -7:] = rows
+    pos = torch.arange(S, device="cuda")[None, None]
+    kw = dict(freqs=dev(co.rope_frequencies(64), torch.float64), q_weight=torch.rand(H, d, device="cuda"))
+    want, _ = trevs.norm_rope(rows, None, pos[:, :, -7:].contiguous(), **kw)
+    trevs.norm_rope(q, None, pos, inplace=True, **kw)
+    assert torch.equal(q[:, -7:], want) and not q[:, :-7].any()
+
+
 # ------------------------------------------------------------ summed weights
 def scores_for(m, c, rng):
     s = trevs.kv8_scores(c)
@@ -532,6 +545,23 @@ def test_beam_select_more_ties_than_the_join_lists():
     score = torch.zeros(2, 64, device="cuda")
     got = trevs.beam_select(torch.zeros(2, 64, 9000, device="cuda"), score, n_out=64)
     assert got[1].tolist() == [[0] * 64] * 2 and got[2].tolist() == [list(range(64))] * 2
+
+
+def test_beam_select_offsets_past_32_bits():
+    """Six rows of 4e8 logits, 4.8 GB."""
+    V = 400_000_000
+    logits = torch.zeros(3, 2, V, dtype=torch.bfloat16, device="cuda")
+    logits[2, 1, V - 1], logits[2, 1, 7], logits[2, 0, V - 5], logits[0, 1, 9], logits[0, 0, 3] = 12.0, 11.0, 10.0, 9.0, 8.0
+    logits[1, 0, V // 2], logits[1, 0, 0] = 3.0, 2.0
+    score = torch.tensor([[0.0, -0.5], [-1.0, -9.0], [0.0, -0.25]], device="cuda")
+    got = trevs.beam_select(logits, score, n_out=2)
+    sums = [[V - 1 + math.exp(8), V - 1 + math.exp(9)], [V - 2 + math.exp(3) + math.exp(2), V],
+            [V - 1 + math.exp(10), V - 2 + math.exp(12) + math.exp(11)]]
+    want = [[(-0.5 + 9, 1, 9), (8.0, 0, 3)], [(-1.0 + 3, 0, V // 2), (-1.0 + 2, 0, 0)], [(-0.25 + 12, 1, V - 1), (-0.25 + 11, 1, 7)]]
+    assert got[1].tolist() == [[w for _, w, _ in row] for row in want]
+    assert got[2].tolist() == [[v for _, _, v in row] for row in want]
+    exact = np.array([[x - math.log(sums[b][w]) for x, w, _ in row] for b, row in enumerate(want)])
+    assert np.all(np.abs(host(got[0]) - exact) <= 80 * 2.0 ** -24 + 2.0 ** -24 * np.abs(exact))
 
 
 # ------------------------------------------------------------------- reorder
