@@ -42,6 +42,10 @@ struct Raw {
 #pragma unroll
     for (int j = 0; j < E::kBytes / 2; ++j) w[j] = ldg16(p + j);
   }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int j = 0; j < E::kBytes / 2; ++j) w[j] = zero4();
+  }
   __device__ __forceinline__ void parts(u32x4 (&out)[kParts<E>]) const {
     if constexpr (E::kBytes == 2) {
       out[0] = w[0];
@@ -421,7 +425,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void many_rows_kernel(Weight
   for (int hk = hg * a.heads; hk < min((hg + 1) * a.heads, a.c.H_kv); ++hk) {
     if (first >= end) break;
     // A thread stages parts of every S-th row: it follows the row's place.  (Dividing the row's number by G
-    // takes as long as the exponentials.)
+    // takes as long as the exponentials; for the log-sum-exps alone it takes 8 of 308 us of 4 x 4259 rows.)
     constexpr int kPer = 256 / S;  // threads of a row, which has kPer * kVecs vectors
     static_assert(kPer * kVecs == D / 8, "whole rows");
     Raw<E> raw[kVecs];
@@ -429,27 +433,36 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void many_rows_kernel(Weight
     const int in_row = tid / kPer, vec = tid % kPer;
     int row = first * S + in_row, g = row % a.G;
     const size_t head = (size_t)b * a.T_max * a.q_ld + (size_t)hk * a.G * D + vec * 8;
-    size_t at = head + (size_t)(row / a.G) * a.q_ld + g * D;
+    const size_t head_lse = ((size_t)b * a.H_q + hk * a.G) * a.T_max;
+    int t = row / a.G;
+    size_t at = head + (size_t)t * a.q_ld + g * D, at_lse = head_lse + (size_t)g * a.T_max + t;
     float base = 0.f;
     int lim = 0;
-    auto load = [&](int stage) {
-      // (a row past the last is the first one: its weights come to nothing, but it may hold anything)
-      const size_t from = row < n_rows ? at : head;
+    auto load = [&] {
+      const bool live = row < n_rows;
 #pragma unroll
-      for (int i = 0; i < kVecs; ++i) raw[i].load(a.q, from + i * (kPer * 8));
+      for (int i = 0; i < kVecs; ++i) raw[i].load(a.q, (live ? at : head) + i * (kPer * 8));
+      base = live ? a.lse[at_lse] : -INFINITY;
+      lim = !live ? 0 : a.causal ? s.L - s.rows + t + 1 : s.L;
       row += S;
       at += step;
       g += S % a.G;
       const bool over = g >= a.G;
       at += over ? wrap : 0;
       g -= over ? a.G : 0;
-      if (tid < S) {
-        const int r = stage * S + tid, t = r / a.G, h = hk * a.G + r - t * a.G;
-        base = r < n_rows ? row_base(a.lse[((size_t)b * a.H_q + h) * a.T_max + t]) : -INFINITY;
-        lim = r >= n_rows ? 0 : a.causal ? s.L - s.rows + t + 1 : s.L;
-      }
+      t += S / a.G + over;
+      at_lse = head_lse + (size_t)g * a.T_max + t;
     };
     auto store = [&](int buf) {
+      // places past the last row are zeros, as are rows that give nothing: products that take no limits drop
+      // them by their base alone, and exp2(NaN - inf) is NaN
+      const bool none = base == -INFINITY;
+      if (__any(none)) {
+        if (none) {
+#pragma unroll
+          for (int i = 0; i < kVecs; ++i) raw[i].clear();
+        }
+      }
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) {
         u32x4 parts[NP];
@@ -458,12 +471,12 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void many_rows_kernel(Weight
         for (int p = 0; p < NP; ++p)
           sh.q[buf][p][in_row * (D / 8) + ((vec + i * kPer) ^ query_swizzle<D>(in_row))] = parts[p];
       }
-      if (tid < S) {
-        reinterpret_cast<float*>(sh.base[buf])[tid] = base;
-        reinterpret_cast<int*>(sh.lim[buf])[tid] = lim;
+      if (vec == 0) {
+        reinterpret_cast<float*>(sh.base[buf])[in_row] = row_base(base);
+        reinterpret_cast<int*>(sh.lim[buf])[in_row] = lim;
       }
     };
-    load(first);
+    load();
     bf16x8 kk[2][D / 16];
     float f[2], sum[2] = {0.f, 0.f};
     {
@@ -483,7 +496,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void many_rows_kernel(Weight
     __syncthreads();
     for (int stage = first; stage < end; ++stage) {
       const int buf = (stage - first) & 1;
-      if (stage + 1 < end) load(stage + 1);
+      if (stage + 1 < end) load();
       // rows see more and more keys: the limits of the stage's first and last one
       const int least = a.causal ? s.L - s.rows + stage * S / a.G + 1 : s.L;
       const int most = a.causal ? s.L - s.rows + min(stage * S + S - 1, n_rows - 1) / a.G + 1 : s.L;
