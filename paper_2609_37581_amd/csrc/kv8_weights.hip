@@ -161,6 +161,18 @@ struct FewRows {
       load(0);
       look_up(1);
     }
+    // rows that give nothing are zeros: exp2(NaN - inf) is NaN (here, not with their loads, which the keys'
+    // would wait for)
+#pragma unroll
+    for (int m = 0; m < NQ; ++m) {
+      const bool none = nl[m] == -INFINITY;
+      if (__any(none)) {
+        if (none) {
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) q[m][c].clear();
+        }
+      }
+    }
 #pragma unroll 1
     for (int u = 0; u < run; ++u) {
       const int j = j0 + 16 * u * Y;

@@ -59,6 +59,16 @@ def test_weights_rows_that_give_nothing(T, H_q, H_kv, d, dtype, value):
     check_rows_that_give_nothing(T, H_q, H_kv, d, dtype, value, 0)
 
 
+@pytest.mark.parametrize("T,H_q,H_kv,d", [(1, 2, 1, 64), (3, 4, 2, 64), (1, 28, 4, 128), (2, 7, 1, 128), (4, 32, 4, 128),
+                                          (3, 8, 1, 256), (1, 20, 10, 64)])
+@pytest.mark.parametrize("max_pages", [0, 512])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_weights_few_rows_that_give_nothing(T, H_q, H_kv, d, max_pages, dtype, value):
+    """The same for the kernels of few rows, under a short table and a long one."""
+    check_rows_that_give_nothing(T, H_q, H_kv, d, dtype, value, max_pages)
+
+
 def check_rows_that_give_nothing(T, H_q, H_kv, d, dtype, value, max_pages):
     rng = np.random.default_rng(T * d)
     m = model(rng, [120, T], 16, H_kv, d)
