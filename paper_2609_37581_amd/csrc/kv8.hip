@@ -262,6 +262,7 @@ __device__ __forceinline__ void move_block(const CacheView& v, int layer, int h,
     static_assert(kItems * B::kThreads == D * kGroups, "whole items");
     u32x4 w[kItems], next[kItems], at16[kItems];
     uint64_t runs = sh.runs;
+    auto below = [](int n) { return (uint32_t)((1ull << (8 * min(max(n, 0), 4))) - 1ull); };  // a word's first n bytes
     auto fetch = [&](int t) {
       const int from = map.block[t];
 #pragma unroll
@@ -291,13 +292,17 @@ __device__ __forceinline__ void move_block(const CacheView& v, int layer, int h,
       for (int i = 0; i < kItems; ++i) {
         const int e = tid + i * B::kThreads, t0 = e % kGroups * 16;
         const uint8_t* row = reinterpret_cast<const uint8_t*>(lds + e / kGroups * B::kRow);
-        // a byte for every token, those of other blocks dropped: the reads wait for nothing
+        // A byte for every token, those of other blocks dropped, a word at a time: the reads wait for nothing.
+        // (With a select to each byte the compiler may put some of the reads behind a branch, as it did for
+        // blocks of 128 x 64: 97 registers instead of 75, 22.5 us instead of 19.4.)
         uint32_t byte[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) byte[j] = row[(at16[i][j >> 2] >> (8 * (j & 3))) & 0xff];
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-          w[i][j >> 2] |= t0 + j >= r0 && t0 + j < r1 ? byte[j] << (8 * (j & 3)) : 0u;
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t word = byte[4 * j] | byte[4 * j + 1] << 8 | byte[4 * j + 2] << 16 | byte[4 * j + 3] << 24;
+          w[i][j] |= word & below(r1 - t0 - 4 * j) & ~below(r0 - t0 - 4 * j);
+        }
       }
       __syncthreads();
       r0 = r1;
@@ -330,8 +335,7 @@ __device__ __forceinline__ void move_block(const CacheView& v, int layer, int h,
         // (one factor after the other: a block of zeros has the smallest scale, and the product of the two
         // passes fp32's range)
         for (int q = 0; q < 4; ++q) x[q] = x[q] * map.scale[t0 + 4 * j + q] * inv;
-        const int n_t = hi - t0 - 4 * j;  // tokens of this word
-        const uint32_t mask = n_t >= 4 ? ~0u : n_t <= 0 ? 0u : (1u << (8 * n_t)) - 1u;
+        const uint32_t mask = below(hi - t0 - 4 * j);
         y[j] = (to_e4m3(x[0], x[1], x[2], x[3]) & mask) | (y[j] & ~mask);
       }
       *to = y;
