@@ -351,7 +351,8 @@ trevs_status validate_evict(const trevs_kv8_cache* c, const trevs_kv8_evict_args
     return TREVS_ERR_INVALID_ARG;
   if (!a->slots && a->B > c->n_slots) return TREVS_ERR_INVALID_ARG;
   if (a->B > TREVS_MAX_PAGE_REQUESTS) return TREVS_ERR_UNSUPPORTED;
-  if ((int64_t)a->B * a->n_keep > INT32_MAX) return TREVS_ERR_UNSUPPORTED;
+  // (places up to a workgroup past the list stay in 32 bits)
+  if ((int64_t)a->B * a->n_keep > INT32_MAX - 1024) return TREVS_ERR_UNSUPPORTED;
   if ((int64_t)c->n_layers * a->B * c->H_kv + a->B > kMaxGroups) return TREVS_ERR_UNSUPPORTED;
   const size_t list = (size_t)a->B * 4;
   const Span out[] = {{a->score, score_bytes(c)}, {a->n_evicted, list}, {a->kept_idx, list * a->n_keep}};
