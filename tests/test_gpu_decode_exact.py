@@ -1,0 +1,80 @@
+"""The decode loop's results where they can be held to less than the general bounds allow: every rank of a
+selection."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import decode_oracle as do
+from paper_2609_37581_amd import trevs
+from test_gpu_cache import dev, host, storage
+from test_gpu_decode import BEAMS
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float32, torch.bfloat16]
+TOL = 80 * 2.0 ** -24  # of a score before it is rounded, as in check_beams
+
+
+def check_every_rank(got, x, s, done, n, eos):
+    """Each returned score is that of the returned beam and token, nothing is returned twice, and what is not
+    returned is no better than the last, by more than the bound."""
+    score, parent, token = host(got[0]), got[1].cpu().numpy(), got[2].cpu().numpy()
+    B, W, V = x.shape
+    want, wp, wt = do.beam_select(x, s, done, n + 1, eos)
+    for b in range(B):
+        for r in range(n):
+            w, v = int(parent[b, r]), int(token[b, r])
+            if (w, v) == (-1, -1):
+                assert (wp[b, r], wt[b, r]) == (-1, -1) and score[b, r] == -math.inf, (b, r)
+                continue
+            own = s[b, w] if s[b, w] < math.inf else -math.inf
+            if done is not None and done[b, w]:
+                assert v == eos
+                exact = own
+            else:
+                top = x[b, w].max()
+                exact = own + (x[b, w, v] - top) - math.log(np.exp(x[b, w] - top).sum()) if np.isfinite(top) else -math.inf
+            assert score[b, r] == exact or abs(score[b, r] - exact) <= TOL + 2.0 ** -24 * abs(exact), (b, r, w, v)
+            # as good as this rank's own, within what either is off by
+            assert exact == want[b, r] or abs(exact - want[b, r]) <= 2 * TOL, (b, r, exact, want[b, r])
+            near = [i for i in range(n + 1) if i != r and want[b, i] > -math.inf and abs(want[b, i] - want[b, r]) <= 2 * TOL
+                    and wp[b, i] != wp[b, r]]
+            if not near:
+                assert (w, v) == (wp[b, r], wt[b, r]), (b, r)
+        pairs = [p for p in zip(parent[b], token[b]) if p != (-1, -1)]
+        assert len(set(pairs)) == len(pairs)
+        assert all(a >= b for a, b in zip(score[b], score[b][1:]))
+
+
+@pytest.mark.parametrize("shape", BEAMS + [(3, 1, 30000, 1, 1), (2, 8, 40001, 1, 0), (1, 64, 4099, 1, 3), (2, 3, 4096, 2, 0),
+                                           (1, 2, 2049, 63, 1), (4, 16, 2048, 33, 0)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_beam_select_every_rank(shape, dtype):
+    B, W, V, n, pad = shape
+    print(f"[every rank] {shape} {dtype}", flush=True)
+    rng = np.random.default_rng(2 * V + W)
+    full, x = storage(rng.normal(size=(B, W, V + pad)) * 3, dtype)
+    logits, x = full[:, :, :V], x[:, :, :V]
+    score, s = storage(-3 * rng.random((B, W)), torch.float32)
+    check_every_rank(trevs.beam_select(logits, score, n_out=n), x, s, None, n, 0)
+    done = rng.random((B, W)) < 0.3
+    eos = int(rng.integers(0, V))
+    check_every_rank(trevs.beam_select(logits, score, dev(done), n_out=n, eos=eos), x, s, done, n, eos)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [1, 3, 16, 64])
+def test_beam_select_best_in_any_place(dtype, n):
+    """The best lie next to each other, at a chunk's end, one to a chunk, or at the end of a row."""
+    rng = np.random.default_rng(n)
+    V = 20003
+    x = rng.normal(size=(4, 2, V))
+    for b, places in enumerate((range(4000, 4000 + n), range(4096 - n // 2, 4096 - n // 2 + n), range(5, V, V // n),
+                                range(V - n, V))):
+        for i, v in enumerate(list(places)[:n]):
+            x[b, (i * 7) % 2, v] = 9.0 + 0.125 * ((i * 5) % 64)
+    logits, x = storage(x, dtype)
+    score, s = storage(np.array([[-0.25, -0.3125]] * 4), torch.float32)
+    check_every_rank(trevs.beam_select(logits, score, n_out=n), x, s, None, n, 0)
