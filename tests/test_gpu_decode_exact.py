@@ -1,5 +1,5 @@
 """The decode loop's results where they can be held to less than the general bounds allow: every rank of a
-selection."""
+selection, logits of one product."""
 import math
 
 import numpy as np
@@ -8,8 +8,8 @@ import torch
 
 from oracle import decode_oracle as do
 from paper_2609_37581_amd import trevs
-from test_gpu_cache import dev, host, storage
-from test_gpu_decode import BEAMS
+from test_gpu_cache import dev, device_cache, host, model, storage
+from test_gpu_decode import BEAMS, scores_for
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +78,52 @@ def test_beam_select_best_in_any_place(dtype, n):
     logits, x = storage(x, dtype)
     score, s = storage(np.array([[-0.25, -0.3125]] * 4), torch.float32)
     check_every_rank(trevs.beam_select(logits, score, n_out=n), x, s, None, n, 0)
+
+
+@pytest.mark.parametrize("T,H_kv,d,max_pages", [(1, 1, 64, 0), (1, 2, 128, 512), (3, 1, 256, 0), (2, 10, 64, 512), (40, 2, 64, 0),
+                                                (70, 1, 128, 0), (33, 1, 256, 0)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_weights_of_single_products(T, H_kv, d, max_pages, dtype):
+    """Rows with one value each: a logit is one product, with all of the row's bits in it."""
+    print(f"[single products] {T} {H_kv} {d} {max_pages} {dtype}", flush=True)
+    rng = np.random.default_rng(T + d)
+    B, G = 2, 2
+    m = model(rng, [90, T + 3], 16, H_kv, d)
+    if max_pages:
+        m.table = [row + [-1] * (max_pages - len(row)) for row in m.table]
+        m.max_pages = max_pages
+    c = device_cache(m)
+    scale = 0.125
+    x = np.zeros((B, T, H_kv * G, d))
+    at = rng.integers(0, d, x.shape[:3])
+    for i in np.ndindex(*x.shape[:3]):
+        b, _, h = i
+        pages = m.table[b][:-(-m.len[b] // 16)]
+        k = m.k[0, pages, h // G, :, at[i]] * m.k_scale[0, pages, h // G][:, None]
+        x[i][at[i]] = (20 + 10 * rng.random()) * rng.choice([-1, 1]) / (scale * np.abs(k).max())
+    q, qs = storage(x, dtype)
+    _, lse, _, _ = m.attention(qs, scale=scale)
+    ld, ls = storage(lse, torch.float32)
+    score, want = scores_for(m, c, rng)
+    old = want.copy()
+    total, short, bound = [np.zeros_like(want) for _ in range(3)]
+    two = q.bfloat16().float() + (q.float() - q.bfloat16().float()).bfloat16().float()
+    two = host(two)  # the rows in two parts
+    for i in np.ndindex(*x.shape[:3]):
+        b, t, h = i
+        n = m.len[b] - T + t + 1
+        j = np.arange(n)
+        page = np.array(m.table[b])[j // 16]
+        z = scale * qs[i][at[i]] * m.k[0, page, h // G, j % 16, at[i]] * m.k_scale[0, page, h // G]
+        e = np.exp(z - ls[b, h, t])
+        total[b, :n] += e
+        short[b, :n] += np.exp(z * (two[i][at[i]] / qs[i][at[i]]) - ls[b, h, t])
+        # the sum of a logit's parts twice, the scale, its product with log2 e and a block's scale, and the difference's
+        # rounding, 2^-24 each (log2 e's own cancels where the two are equal: once more for each); the exponential 2^-22
+        bound[b, :n] += e * ((8 * np.abs(z) + 3 * abs(ls[b, h, t])) * 2.0 ** -24 + 2.0 ** -22)
+    want += total
+    bound += (T * H_kv * G + 4) * 2.0 ** -24 * (total + bound) + 2.0 ** -23 * (np.abs(old) + np.abs(want))
+    assert dtype == torch.bfloat16 or (np.abs(short - total) > 2 * bound).any()  # a lost third part shows
+    trevs.kv8_weights(c, q, ld, score, scale=scale)
+    err = np.abs(host(score) - want)
+    assert np.all(err <= bound), (err / np.maximum(bound, 1e-300)).max()
