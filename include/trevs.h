@@ -608,10 +608,11 @@ trevs_status trevs_kv8_weights(const trevs_kv8_cache* cache, const trevs_kv8_wei
  * slots.  From there on the kept rows go to free pages, the lowest ones first, in
  * ascending order, their blocks rounded to scales of their own (rows of absent pages
  * are zeros), and the slot gives up the pages that held them; those are free after
- * the call, not for its later requests.  Requests are served in order; one that the
- * free pages do not cover, that names a slot out of range or an earlier request's
- * slot, or whose slot has no more than n tokens, changes nothing.  n_evicted[b] is
- * L - n, or 0; kept_idx[b] lists the kept tokens' old places, ascending, then -1
+ * the call, not for its later requests.  So a call needs the pages of what it
+ * moves to be free: up to n_keep tokens' a request.  Requests are served in order;
+ * one that the free pages do not cover, that names a slot out of range or an earlier
+ * request's slot, or whose slot has no more than n tokens, changes nothing.
+ * n_evicted[b] is L - n, or 0; kept_idx[b] lists the kept tokens' old places, ascending, then -1
  * (-1 throughout where nothing was evicted).  The call must not run beside another
  * one on the same cache. */
 typedef struct trevs_kv8_evict_args {

@@ -1111,7 +1111,9 @@ class Kv8Evict:
     every layer.  Tables, lengths, counts and scores follow.  call() returns
     (n_evicted [B], kept_idx [B,n_keep]): how many tokens went (0: the sequence
     is short enough, or the free pages did not suffice), and the places that the
-    kept ones had, -1 past them or where nothing went."""
+    kept ones had, -1 past them or where nothing went.  Kept tokens move to pages
+    that are free before the call, up to n_keep tokens' a sequence: evict while
+    there is that room."""
 
     def __init__(self, cache, score, slots=None, *, n_keep, n_first=0, n_last=0, keep=None, n=None):
         dev = cache.device

@@ -1,5 +1,5 @@
 """The decode loop's results where they can be held to less than the general bounds allow: every rank of a
-selection, logits of one product."""
+selection, logits of one product, a loop of beams that finish."""
 import math
 
 import numpy as np
@@ -127,3 +127,37 @@ def test_weights_of_single_products(T, H_kv, d, max_pages, dtype):
     trevs.kv8_weights(c, q, ld, score, scale=scale)
     err = np.abs(host(score) - want)
     assert np.all(err <= bound), (err / np.maximum(bound, 1e-300)).max()
+
+
+def test_beams_that_finish():
+    """A loop that goes on until its beams have ended, `done` following the beams: against a search that keeps
+    whole sequences."""
+    rng = np.random.default_rng(17)
+    B, W, V, eos, steps = 3, 4, 11, 2, 9
+    table, x = storage(rng.normal(size=(V, V)) * 2 + 1.5 * (np.arange(V) == eos), torch.float32)  # logits after a token
+    table_lp = x - np.log(np.exp(x).sum(-1, keepdims=True))
+    beam = torch.full((B, W), -math.inf, device="cuda")
+    beam[:, 0] = 0.0
+    token = dev(rng.integers(3, V, (B, 1))).expand(B, W).contiguous()
+    start = token[:, 0].tolist()
+    done = torch.zeros(B, W, dtype=torch.int32, device="cuda")
+    seqs = [[[] for _ in range(W)] for _ in range(B)]
+    plain = [[(0.0, [], False)] for _ in range(B)]
+    for _ in range(steps):
+        logits = table[token.clamp(min=0).long()]
+        beam, parent, token = trevs.beam_select(logits, beam, done, n_out=W, eos=eos)
+        done = done.gather(1, parent.clamp(min=0).long()) | (token == eos).int()
+        seqs = [[seqs[b][p] + [t] for p, t in zip(parent[b].tolist(), token[b].tolist())] for b in range(B)]
+        for b in range(B):
+            more = []
+            for s, seq, over in plain[b]:
+                last = seq[-1] if seq else start[b]
+                more += [(s, seq + [eos], True)] if over else [(s + table_lp[last, v], seq + [v], v == eos) for v in range(V)]
+            plain[b] = sorted(more, key=lambda c: -c[0])[:W]
+            gaps = [p[0] - q[0] for p, q in zip(plain[b], plain[b][1:])]
+            assert min(gaps) > 1e-4  # (no rank is in doubt)
+    for b in range(B):
+        assert seqs[b] == [seq for _, seq, _ in plain[b]]
+        assert done[b].tolist() == [int(over) for _, _, over in plain[b]]
+        assert np.abs(host(beam[b]) - [s for s, _, _ in plain[b]]).max() <= steps * (TOL + 2.0 ** -24 * 40)
+    assert done.all()
