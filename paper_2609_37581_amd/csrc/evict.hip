@@ -4,7 +4,8 @@
 // One workgroup to a sequence: the choice is a stable top-K over keys held in
 // registers, E of them a thread, in which the tokens that always stay have the largest
 // key and NaN the smallest.  Bound by latency: a count and a barrier for each bit of the
-// key.  Sequences of more than 32,768 tokens read the scores again for each bit.
+// key.  Sequences of more than 32,768 tokens read the scores again for each bit (four of
+// 20 k to 32 k tokens 35 us, of 34 k to 60 k 280).
 #include "cache.hpp"
 #include "select.hpp"
 

@@ -102,8 +102,14 @@ __device__ __forceinline__ void load_keys(const WeightsArgs& a, const Places& at
 // of 16.  Bound by the keys' bytes: a wave's rows stay in its registers over the blocks
 // of a sequence, pages are looked up two blocks ahead and keys loaded one, where there
 // are registers for two (one token of 64 sequences of 1.2 k to 16.5 k tokens, 28/4
-// heads of 128: 62 us, 4.7 TB/s; with the keys of one block 66, streamed past the
-// caches 68, as products of 32 x 32, 32 bytes of each of 32 keys, 83).
+// heads of 128: 60 us, 4.9 TB/s; beside 62, with the keys of one block 66, streamed past
+// the caches 68, as products of 32 x 32, 32 bytes of each of 32 keys, 83).  In fp32 two
+// waves share a SIMD and wait for half of their time (32 sequences of 1 k to 8 k tokens:
+// 22 us, 3.4 TB/s; matrix cores busy for 15 % of the cycles, vector units for 39 %).
+// Two tiles of 256 channels spill 20 to 41 registers: 3 or 4 rows of 8 sequences of 8 k to
+// 12 k tokens, 8/1 heads, take 18 us, with the kernel of many rows 14.5; of 2 sequences of
+// 2 k to 3 k 4.2 (16 tokens a workgroup) and 8.1; one row of 8 of 4 k to 8 k, 320/10 heads,
+// 43 and 50.
 constexpr int kRun = 8;  // blocks whose sums are joined at once
 
 // The calling wave's part of the sums of `run` blocks of 16 Y tokens from j0 on.
@@ -360,10 +366,11 @@ __global__ __launch_bounds__(64 * WAVES, (kFewPerCu<E, D, WAVES, NQ> * WAVES / 4
 // A workgroup's four waves hold 64 keys each, widened once into registers, while the
 // query rows of a group, r = t G + g, pass by, staged in LDS a step ahead.  Its sums are
 // one of the parts of its keys' scores, joined by sum_kernel.  Bound by the vector units
-// and the matrix cores one after the other: of a pass over prompts of 4 x 4259 rows with
-// 28/4 heads of 128 (325 us, 800 TFLOP/s) the former are busy 58 % of the cycles, a third
-// of that with exponentials, the latter 43 %, and hardly any at the same time, also where
-// the exponentials of one product are placed among the instructions of the next (344 us).
+// and the matrix cores, half of the time one after the other: of a pass over prompts of
+// 4 x 4259 rows with 28/4 heads of 128 (303 us, 860 TFLOP/s) the former are busy for 57 %
+// of the cycles, a third of that with exponentials, the latter for 41 %, and one or the
+// other for 80 %.  (The exponentials of one product placed among the instructions of the
+// next: 344 us beside 330.)
 
 // Permutation of a staged row's 16-byte columns, by the row's low bits reversed: 16 lanes
 // next to each other read one column of 16 rows, or write 4 or 8 columns of 4 or 2 rows,
@@ -628,8 +635,8 @@ WeightsPlan weights_plan(int B, int T_max, int H_kv, int G, int kv_max, int dtyp
   p.pieces = 1;
   if (p.few) return p;
   // Two workgroups of a CU at once, and as many again for those that see fewer rows (with twice as many prompts
-  // of 4 x 2048 rows with 8/1 heads of 256 take 94 us for 83, of 28/4 of 128 in fp32 104 for 103, the others
-  // the same); the parts' floats: 64 MB at most, where splitting the heads alone does not pass that.
+  // of 4 x 2048 rows with 8/1 heads of 256 take 87 us for 75, of 2 x 2048 with 28/4 of 128 in fp32 115 for 106, of
+  // 4 x 4259 in bf16 300 for 308); the parts' floats: 64 MB at most, where splitting the heads alone does not pass that.
   const long long row_tiles = (n_rows + kRows - 1) / kRows, want = 1024;
   const long long most = std::max((16LL << 20) / ((long long)B * kv_max), 1LL);
   if (most < H_kv) {
